@@ -1,0 +1,193 @@
+/*
+ * dte_train.h -- trainer-side operators around the flat shard, for AMD
+ * Instinct MI355X (gfx950): the two vocabulary tables' lookup, loss and
+ * gradients, and the Muon step of matrices.
+ *
+ * A trainer's step makes the state that dte_extract_delta reads.  These
+ * calls are the parts of it that touch the vocabulary tables and the matrix
+ * optimizer: the embedding's rows and its gradient by sorted tokens; the
+ * per-token loss of a linear layer over a large vocabulary, in pieces of the
+ * vocabulary and without keeping the logits, and its gradients; a matrix
+ * orthogonalised by Newton-Schulz products, and the Muon step built on it,
+ * whose inverse dte_extract_delta computes (see dte_muon_forward).
+ *
+ * Conventions of dte.h apply: device pointers unless stated otherwise, every
+ * buffer owned by the caller, work only enqueued on `stream` (no allocation,
+ * no host synchronisation), argument errors before anything is enqueued, no
+ * exception or abort across the interface.  Results do not depend on timing:
+ * repeated calls on the same inputs write identical bytes (no floating-point
+ * atomics).  Buffers of one call do not overlap except where stated.
+ *
+ * Matrices are row-major with a row stride (`_ld`, in elements, at least the
+ * row length, below 2^22).  Any element alignment is accepted; rows that
+ * begin at 16-byte addresses (base and stride) are read and written in
+ * 16-byte accesses.  `workspace` is device memory, 256-byte aligned, of at
+ * least the bytes that the operator's _workspace_bytes call returns for the
+ * same arguments (-1: invalid arguments); its contents need not be kept
+ * between calls, and calls that overlap on one workspace race.
+ */
+#ifndef DTE_TRAIN_H
+#define DTE_TRAIN_H
+
+#include <stdint.h>
+
+#include "dte.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+/* Element types. */
+#define DTE_TYPE_F32 0  /* IEEE binary32 */
+#define DTE_TYPE_BF16 1 /* bfloat16 */
+
+#define DTE_MAX_NS_STEPS 16
+
+/* Rows of an embedding table: out[i, :] = scale * table[ids[i], :], products
+ * in binary32, rounded once (nearest even) where `type` is BF16.  An id
+ * outside [0, vocab) is padding: its row is zero.
+ * table: [vocab, hidden] of `type`; ids: int64[n]; out: [n, hidden] of
+ * `type`.  n == 0 or hidden == 0 enqueues nothing.
+ * Errors: DTE_ERR_ARG (null pointer, negative size, unknown type, a row
+ * stride below `hidden` or not below 2^22, n or vocab above 2^31 - 65537, a
+ * scale that is not finite),
+ * DTE_ERR_HIP. */
+dte_status dte_embedding_forward(const void* table, int32_t type, int64_t vocab, int64_t hidden,
+                                 int64_t table_ld, const int64_t* ids, int64_t n, float scale,
+                                 void* out, int64_t out_ld, void* stream);
+
+/* Workspace of dte_embedding_backward (or -1). */
+int64_t dte_embedding_workspace_bytes(int64_t n, int64_t vocab, int64_t hidden);
+
+/* The table's gradient: table_grad[v, :] = scale * sum over i with
+ * ids[i] == v of grad[i, :], padding ids left out.  The ids are sorted, each
+ * token's rows summed in ascending i in binary32 (runs of a frequent token
+ * in pieces of fixed length, joined in order) and rounded once.
+ * grad: [n, hidden] of grad_type; table_grad: [vocab, hidden] of table_type,
+ * every row written (zeros for tokens that do not occur); with accumulate
+ * != 0 (F32 tables only) the sums are added to its contents and the rows of
+ * other tokens are neither read nor written.
+ * Errors: as dte_embedding_forward; DTE_ERR_ARG also for accumulate with a
+ * BF16 table and for a missing, small or misaligned workspace. */
+dte_status dte_embedding_backward(const void* grad, int32_t grad_type, int64_t grad_ld,
+                                  const int64_t* ids, int64_t n, int64_t vocab, int64_t hidden,
+                                  float scale, void* table_grad, int32_t table_type,
+                                  int64_t table_ld, int32_t accumulate, void* workspace,
+                                  int64_t workspace_bytes, void* stream);
+
+/* A linear layer over the vocabulary and the targets of its tokens:
+ *   z[t, v] = scale * sum_k hidden[t, k] weight[v, k]
+ * hidden: BF16 [tokens, dim]; weight: BF16 [vocab, dim]; targets:
+ * int64[tokens]; scale: finite (the inverse of a sampling temperature).  A
+ * target outside [0, vocab) marks a padding token: it has no loss and no
+ * gradient, and its hidden row, which may hold anything, is not used.
+ * 0 <= tokens < 2^31 - 512, 1 <= vocab < 2^31 - 512, 1 <= dim < 2^20. */
+typedef struct {
+    const uint16_t* hidden;
+    const uint16_t* weight;
+    const int64_t* targets;
+    int64_t hidden_ld;
+    int64_t weight_ld;
+    int64_t tokens;
+    int64_t vocab;
+    int64_t dim;
+    float scale;
+    int32_t reserved; /* 0 */
+} dte_linear_ce;
+
+/* Workspace of dte_linear_ce_forward (backward == 0) or
+ * dte_linear_ce_backward with a weight gradient of grad_type (backward !=
+ * 0); -1 for invalid arguments.  Only the sizes, strides and the alignment
+ * of `weight` are looked at. */
+int64_t dte_linear_ce_workspace_bytes(const dte_linear_ce* c, int32_t backward,
+                                      int32_t grad_type);
+
+/* Per-token loss (negative log-probability of the target) and log-sum-exp:
+ *   lse[t] = log sum_v exp z[t, v],  loss[t] = lse[t] - z[t, targets[t]]
+ * (both 0 for padding).  Products of BF16 values are exact and summed in
+ * binary32; maximum and sum of the softmax are kept per piece of the
+ * vocabulary in binary32 and joined; the logits are not stored.
+ * loss, lse: float[tokens].  Errors: DTE_ERR_ARG, DTE_ERR_HIP. */
+dte_status dte_linear_ce_forward(const dte_linear_ce* c, float* loss, float* lse,
+                                 void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Gradients for one weight per token's loss (the derivative of the caller's
+ * objective by loss[t]; for a policy gradient the token's advantage):
+ *   G[t, v] = scale * grad_loss[t] * (exp(z[t, v] - lse[t]) - [v == targets[t]])
+ *   grad_hidden = G weight,  grad_weight = G^T hidden
+ * z is computed again, piece by piece of the vocabulary.  G is rounded to
+ * BF16 once where the result is BF16; for a binary32 grad_weight it is kept
+ * in three BF16 terms (24 bits).  Sums are in binary32.
+ * lse: as dte_linear_ce_forward wrote it; grad_loss: float[tokens].
+ * grad_hidden: BF16 [tokens, dim], zero for padding; grad_weight: [vocab,
+ * dim] of grad_type, every element written; with accumulate != 0 (F32 only)
+ * the gradient is added to its contents.  Either may be NULL (not wanted).
+ * Errors: DTE_ERR_ARG, DTE_ERR_HIP. */
+dte_status dte_linear_ce_backward(const dte_linear_ce* c, const float* lse,
+                                  const float* grad_loss, uint16_t* grad_hidden,
+                                  int64_t grad_hidden_ld, void* grad_weight, int32_t grad_type,
+                                  int64_t grad_weight_ld, int32_t accumulate, void* workspace,
+                                  int64_t workspace_bytes, void* stream);
+
+/* A Newton-Schulz iteration: X_0 = x / (|x|_F + eps), then for k < steps
+ *   X <- a_k X + b_k S X + c_k S S X,  S = X X^T
+ * (on the smaller side), coefficients[k] = {a_k, b_k, c_k}.  The quintic
+ * pushes singular values towards one.  1 <= steps <= DTE_MAX_NS_STEPS, eps
+ * >= 0 finite; coefficients finite and such that the polynomials keep
+ * singular values that start in [0, 1] at or below 16 (checked). */
+typedef struct {
+    int32_t steps;
+    int32_t reserved; /* 0 */
+    double eps;
+    double coefficients[DTE_MAX_NS_STEPS][3];
+} dte_newton_schulz;
+
+/* Workspace of dte_orthogonalise and dte_muon_forward (or -1). */
+int64_t dte_orthogonalise_workspace_bytes(int64_t batch, int64_t rows, int64_t cols);
+
+/* Orthogonalise a batch of matrices: out[b] = X_steps of x[b].
+ * Products run on FP16 operands (11 bits, scaled by powers of two that the
+ * bound on the singular values gives) with binary32 sums; X itself is kept
+ * in binary32 from step to step.  The Frobenius norm is summed in binary64.
+ * x: [batch, rows, cols] of x_type, strides x_ld and x_stride (elements
+ * between matrices); out: BF16 likewise, rounded once.  rows, cols below
+ * 2^16; batch below 2^16.  A zero matrix stays zero (with eps > 0).
+ * Errors: DTE_ERR_ARG, DTE_ERR_HIP. */
+dte_status dte_orthogonalise(const void* x, int32_t x_type, int64_t batch, int64_t rows,
+                             int64_t cols, int64_t x_ld, int64_t x_stride,
+                             const dte_newton_schulz* ns, uint16_t* out, int64_t out_ld,
+                             int64_t out_stride, void* workspace, int64_t workspace_bytes,
+                             void* stream);
+
+/* One Muon step of a batch of matrices. */
+typedef struct {
+    double lr;           /* >= 0, finite */
+    double momentum;     /* 0 <= momentum < 1 */
+    double weight_decay; /* decoupled; 1 - lr*weight_decay > 0 */
+    double update_scale; /* finite; multiplies the orthogonal update */
+    int32_t nesterov;    /* != 0: the update looks one momentum step ahead */
+    int32_t reserved;    /* 0 */
+    dte_newton_schulz ns;
+} dte_muon_step;
+
+/* In place on contiguous [batch, rows, cols] binary32 p and momentum, with
+ * gradient g:
+ *   M = mu*M + g;  U = nesterov ? g + mu*M : M;  O = BF16(orthogonalised U)
+ *   p = decay*p - rate*O      decay = 1 - lr*weight_decay, rate = lr*update_scale
+ * (mu, decay and rate rounded once from binary64; binary32, left to right,
+ * no fused multiply-add).  update: BF16 [batch, rows, cols], receives O.
+ * The step can be inverted without a snapshot: O is a function of M (and of
+ * g with nesterov), and dte_extract_delta with m = O (as binary32), v = 1,
+ * beta1 = beta2 = 0, eps = 0, lr = rate and weight_decay such that 1 -
+ * lr*weight_decay = decay computes theta_hat = (theta + rate*O) / decay.
+ * Errors: DTE_ERR_ARG, DTE_ERR_HIP. */
+dte_status dte_muon_forward(float* p, float* momentum, const float* g, int64_t batch,
+                            int64_t rows, int64_t cols, const dte_muon_step* hp,
+                            uint16_t* update, void* workspace, int64_t workspace_bytes,
+                            void* stream);
+
+#ifdef __cplusplus
+}
+#endif
+
+#endif /* DTE_TRAIN_H */

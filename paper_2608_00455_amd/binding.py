@@ -1,4 +1,4 @@
-"""ctypes binding of libdte.so (include/dte.h): same names, argument
+"""ctypes binding of libdte.so (include/dte.h, dte_train.h): same names, argument
 marshalling only.  Device buffers are passed as integer addresses (for
 example torch.Tensor.data_ptr()), streams as integer hipStream_t handles
 (torch.cuda.current_stream().cuda_stream); every step runs in the library.
@@ -15,12 +15,18 @@ DTE_OK, DTE_ERR_ARG, DTE_ERR_PLAN, DTE_ERR_CAPACITY, DTE_ERR_HIP = 0, 1, 2, 3, 4
 DTE_ERR_IO, DTE_ERR_CORRUPT, DTE_ERR_CHAIN, DTE_ERR_UNSUPPORTED, DTE_ERR_HOST = 5, 6, 7, 8, 9
 DTE_MAX_DIMS = 4
 DTE_MAX_RANKS = 64
+DTE_TYPE_F32, DTE_TYPE_BF16 = 0, 1
+DTE_MAX_NS_STEPS = 16
 
 EXPORTED = ("dte_derive_scalars", "dte_extract_delta", "dte_ordered_workspace_bytes",
             "dte_extract_delta_ordered", "dte_extract_delta_ordered_noalloc",
             "dte_ordered_noalloc_max_capacity", "dte_plan_create", "dte_plan_destroy",
             "dte_plan_info", "dte_remap", "dte_extract_remap", "dte_apply", "dte_remap_apply",
-            "dte_extract_remap_apply", "dte_extract_runs", "dte_adamw_forward", "dte_status_string")
+            "dte_extract_remap_apply", "dte_extract_runs", "dte_adamw_forward", "dte_status_string",
+            # include/dte_train.h
+            "dte_embedding_forward", "dte_embedding_workspace_bytes", "dte_embedding_backward",
+            "dte_linear_ce_workspace_bytes", "dte_linear_ce_forward", "dte_linear_ce_backward",
+            "dte_orthogonalise_workspace_bytes", "dte_orthogonalise", "dte_muon_forward")
 
 
 class DteError(RuntimeError):
@@ -61,6 +67,27 @@ class dte_op(ctypes.Structure):
                 ("extent", ctypes.c_int64 * DTE_MAX_DIMS),
                 ("dst_origin", ctypes.c_int64 * DTE_MAX_DIMS),
                 ("dst_shape", ctypes.c_int64 * DTE_MAX_DIMS)]
+
+
+class dte_linear_ce(ctypes.Structure):
+    _fields_ = [("hidden", ctypes.c_void_p), ("weight", ctypes.c_void_p),
+                ("targets", ctypes.c_void_p), ("hidden_ld", ctypes.c_int64),
+                ("weight_ld", ctypes.c_int64), ("tokens", ctypes.c_int64),
+                ("vocab", ctypes.c_int64), ("dim", ctypes.c_int64), ("scale", ctypes.c_float),
+                ("reserved", ctypes.c_int32)]
+
+
+class dte_newton_schulz(ctypes.Structure):
+    _fields_ = [("steps", ctypes.c_int32), ("reserved", ctypes.c_int32),
+                ("eps", ctypes.c_double),
+                ("coefficients", (ctypes.c_double * 3) * DTE_MAX_NS_STEPS)]
+
+
+class dte_muon_step(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_double), ("momentum", ctypes.c_double),
+                ("weight_decay", ctypes.c_double), ("update_scale", ctypes.c_double),
+                ("nesterov", ctypes.c_int32), ("reserved", ctypes.c_int32),
+                ("ns", dte_newton_schulz)]
 
 
 _L = None
@@ -123,6 +150,29 @@ def _lib():
                                 ctypes.POINTER(I64), P]
         L.dte_adamw_forward.restype = S
         L.dte_adamw_forward.argtypes = [P, P, P, P, I64, ctypes.POINTER(dte_adamw_step), P]
+        F32 = ctypes.c_float
+        ce_p = ctypes.POINTER(dte_linear_ce)
+        L.dte_embedding_forward.restype = S
+        L.dte_embedding_forward.argtypes = [P, I32, I64, I64, I64, P, I64, F32, P, I64, P]
+        L.dte_embedding_workspace_bytes.restype = I64
+        L.dte_embedding_workspace_bytes.argtypes = [I64, I64, I64]
+        L.dte_embedding_backward.restype = S
+        L.dte_embedding_backward.argtypes = [P, I32, I64, P, I64, I64, I64, F32, P, I32, I64, I32,
+                                             P, I64, P]
+        L.dte_linear_ce_workspace_bytes.restype = I64
+        L.dte_linear_ce_workspace_bytes.argtypes = [ce_p, I32, I32]
+        L.dte_linear_ce_forward.restype = S
+        L.dte_linear_ce_forward.argtypes = [ce_p, P, P, P, I64, P]
+        L.dte_linear_ce_backward.restype = S
+        L.dte_linear_ce_backward.argtypes = [ce_p, P, P, P, I64, P, I32, I64, I32, P, I64, P]
+        L.dte_orthogonalise_workspace_bytes.restype = I64
+        L.dte_orthogonalise_workspace_bytes.argtypes = [I64, I64, I64]
+        L.dte_orthogonalise.restype = S
+        L.dte_orthogonalise.argtypes = [P, I32, I64, I64, I64, I64, I64,
+                                        ctypes.POINTER(dte_newton_schulz), P, I64, I64, P, I64, P]
+        L.dte_muon_forward.restype = S
+        L.dte_muon_forward.argtypes = [P, P, P, I64, I64, I64, ctypes.POINTER(dte_muon_step), P, P,
+                                       I64, P]
         _L = L
     return _L
 
@@ -271,3 +321,64 @@ def dte_apply(plan, shards, off, val, rank_count, rank_capacity, stream=0):
 def raw_status(fn: str, *args) -> int:
     """Call an entry point and return its raw status (for error-path tests)."""
     return getattr(_lib(), fn)(*args)
+
+
+# ---- include/dte_train.h ---------------------------------------------------
+
+def dte_embedding_forward(table, type, vocab, hidden, table_ld, ids, n, scale, out, out_ld,
+                          stream=0):
+    _check("dte_embedding_forward",
+           _lib().dte_embedding_forward(table or None, type, vocab, hidden, table_ld, ids or None,
+                                        n, scale, out or None, out_ld, stream or None))
+
+
+def dte_embedding_workspace_bytes(n, vocab, hidden) -> int:
+    return int(_lib().dte_embedding_workspace_bytes(n, vocab, hidden))
+
+
+def dte_embedding_backward(grad, grad_type, grad_ld, ids, n, vocab, hidden, scale, table_grad,
+                           table_type, table_ld, accumulate, workspace, workspace_bytes, stream=0):
+    _check("dte_embedding_backward",
+           _lib().dte_embedding_backward(grad or None, grad_type, grad_ld, ids or None, n, vocab,
+                                         hidden, scale, table_grad or None, table_type, table_ld,
+                                         accumulate, workspace or None, workspace_bytes,
+                                         stream or None))
+
+
+def dte_linear_ce_workspace_bytes(c, backward, grad_type=DTE_TYPE_F32) -> int:
+    return int(_lib().dte_linear_ce_workspace_bytes(ctypes.byref(c), backward, grad_type))
+
+
+def dte_linear_ce_forward(c, loss, lse, workspace, workspace_bytes, stream=0):
+    _check("dte_linear_ce_forward",
+           _lib().dte_linear_ce_forward(ctypes.byref(c), loss or None, lse or None,
+                                        workspace or None, workspace_bytes, stream or None))
+
+
+def dte_linear_ce_backward(c, lse, grad_loss, grad_hidden, grad_hidden_ld, grad_weight, grad_type,
+                           grad_weight_ld, accumulate, workspace, workspace_bytes, stream=0):
+    _check("dte_linear_ce_backward",
+           _lib().dte_linear_ce_backward(ctypes.byref(c), lse or None, grad_loss or None,
+                                         grad_hidden or None, grad_hidden_ld, grad_weight or None,
+                                         grad_type, grad_weight_ld, accumulate, workspace or None,
+                                         workspace_bytes, stream or None))
+
+
+def dte_orthogonalise_workspace_bytes(batch, rows, cols) -> int:
+    return int(_lib().dte_orthogonalise_workspace_bytes(batch, rows, cols))
+
+
+def dte_orthogonalise(x, x_type, batch, rows, cols, x_ld, x_stride, ns, out, out_ld, out_stride,
+                      workspace, workspace_bytes, stream=0):
+    _check("dte_orthogonalise",
+           _lib().dte_orthogonalise(x or None, x_type, batch, rows, cols, x_ld, x_stride,
+                                    ctypes.byref(ns), out or None, out_ld, out_stride,
+                                    workspace or None, workspace_bytes, stream or None))
+
+
+def dte_muon_forward(p, momentum, g, batch, rows, cols, hp, update, workspace, workspace_bytes,
+                     stream=0):
+    _check("dte_muon_forward",
+           _lib().dte_muon_forward(p or None, momentum or None, g or None, batch, rows, cols,
+                                   ctypes.byref(hp), update or None, workspace or None,
+                                   workspace_bytes, stream or None))

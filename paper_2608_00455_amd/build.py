@@ -14,7 +14,8 @@ import tempfile
 HERE = os.path.dirname(os.path.abspath(__file__))
 SRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libdte.so")
-SOURCES = ["dte_api.hip", "extract.hip", "remap.hip", "store.hip"]
+SOURCES = ["dte_api.hip", "extract.hip", "remap.hip", "store.hip",
+           "embedding.hip", "linear_ce.hip", "orthogonalise.hip"]
 CEIL_LIB = os.path.join(HERE, "libceilings.so")
 CEIL_SOURCES = ["ceilings.hip"]
 
@@ -31,13 +32,23 @@ def hipcc():
     return os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 
+def _run(cmds):
+    procs = [(c, subprocess.Popen(c)) for c in cmds]
+    failed = [(p.returncode, c) for c, p in procs if p.wait() != 0]
+    if failed:
+        raise subprocess.CalledProcessError(*failed[0])
+
+
 def build(extra=()):
-    cmds = [[hipcc()] + HIPCC_FLAGS + list(extra) + ["-o", out] + [os.path.join(SRC, s) for s in srcs]
-            for out, srcs in ((LIB, SOURCES), (CEIL_LIB, CEIL_SOURCES))]
-    procs = [subprocess.Popen(c) for c in cmds]
-    for p, c in zip(procs, cmds):
-        if p.wait() != 0:
-            raise subprocess.CalledProcessError(p.returncode, c)
+    """Compile every source (in parallel), then link the two libraries."""
+    flags = HIPCC_FLAGS + list(extra)
+    with tempfile.TemporaryDirectory() as tmp:
+        obj = {s: os.path.join(tmp, s.replace(".hip", ".o")) for s in SOURCES + CEIL_SOURCES}
+        compile_flags = [f for f in flags if f != "-shared"]
+        _run([[hipcc()] + compile_flags + ["-c", os.path.join(SRC, s), "-o", o]
+              for s, o in obj.items()])
+        _run([[hipcc()] + flags + ["-o", out] + [obj[s] for s in srcs]
+              for out, srcs in ((LIB, SOURCES), (CEIL_LIB, CEIL_SOURCES))])
     return LIB
 
 

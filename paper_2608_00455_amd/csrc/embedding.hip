@@ -1,0 +1,674 @@
+// Embedding rows and the table's gradient (include/dte_train.h).  Both only
+// move memory: the forward reads and writes n rows, the gradient reads n rows
+// and writes the table (or reads and writes the rows that occur).
+//
+// Gradient: the ids are sorted with their positions (stable radix sort, two
+// passes of 9 bits for a vocabulary below 2^18), so that a token's rows are
+// consecutive and in ascending position.  The sorted list is cut into chunks
+// of equal length; a block sums the runs of its chunk in registers, one pass
+// over the rows.  A run that lies inside the chunk is finished there; a run
+// that crosses a border leaves a binary32 partial row, and a second kernel
+// joins the partials in order.  So a frequent token (a run of thousands) is
+// spread over many blocks, no sum depends on timing, and there are no
+// floating-point atomics.  Rows of tokens that do not occur are written by
+// further blocks of the same launch.
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+
+#include "abi_guard.h"
+#include "train_common.h"
+
+namespace dte {
+namespace {
+
+using namespace tr;
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+// ---- forward ------------------------------------------------------------------
+
+// kCols columns of a thread: contiguous (16 bytes) or, where rows do not
+// begin at 16-byte addresses, strided by the wave.
+template <typename T>
+struct Row;
+template <>
+struct Row<float> {
+    static constexpr int kCols = 4;
+    static __device__ __forceinline__ float value(float x) { return x; }
+    static __device__ __forceinline__ float make(float x) { return x; }
+};
+template <>
+struct Row<uint16_t> {
+    static constexpr int kCols = 8;
+    static __device__ __forceinline__ float value(uint16_t x) { return from_bf16(x); }
+    static __device__ __forceinline__ uint16_t make(float x) { return to_bf16(x); }
+};
+
+constexpr int kSegVecs = 256;      // vectors of a row that one wave takes: 4 per lane
+
+template <typename T, bool kAligned>
+__global__ __launch_bounds__(256) void embedding_rows_kernel(const T* table, int64_t vocab,
+                                                             int64_t hidden, int64_t table_ld,
+                                                             const int64_t* ids, int64_t n,
+                                                             float scale, T* out, int64_t out_ld,
+                                                             int32_t segs)
+{
+    constexpr int kCols = Row<T>::kCols;
+    const int lane = threadIdx.x & 63;
+    const int64_t unit = (int64_t)blockIdx.x * 4 +
+                         __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t r = unit / segs;
+    const int32_t seg = (int32_t)(unit - r * segs);
+    if (r >= n) return;
+    const int64_t id = ids[r];
+    const bool ok = id >= 0 && id < vocab;
+    const T* src = table + (ok ? id : 0) * table_ld;
+    T* dst = out + r * out_ld;
+    if constexpr (kAligned) {
+        typedef T vec __attribute__((ext_vector_type(kCols)));
+        const int64_t c0 = (int64_t)seg * kSegVecs * kCols + lane * kCols;
+        vec x[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int64_t c = c0 + k * 64 * kCols;
+            x[k] = ok && c < hidden ? *(const vec*)(src + c) : vec(0);
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int64_t c = c0 + k * 64 * kCols;
+            if (c >= hidden) break;
+            vec y;
+#pragma unroll
+            for (int i = 0; i < kCols; ++i)
+                y[i] = ok ? Row<T>::make(scale * Row<T>::value(x[k][i])) : T(0);
+            *(vec*)(dst + c) = y;
+        }
+    } else {
+        const int64_t c0 = (int64_t)seg * kSegVecs * kCols;
+#pragma unroll 4
+        for (int k = 0; k < 4 * kCols; ++k) {
+            const int64_t c = c0 + k * 64 + lane;
+            if (c >= hidden) break;
+            dst[c] = ok ? Row<T>::make(scale * Row<T>::value(src[c])) : T(0);
+        }
+    }
+}
+
+template <typename T>
+hipError_t launch_rows(const void* table, int64_t vocab, int64_t hidden, int64_t table_ld,
+                       const int64_t* ids, int64_t n, float scale, void* out, int64_t out_ld,
+                       hipStream_t st)
+{
+    const int64_t segs = div_up(hidden, (int64_t)kSegVecs * Row<T>::kCols);
+    const int64_t blocks = div_up(n * segs, 4);
+    if (blocks > 0x7fffffff) return hipErrorInvalidValue;
+    const bool aligned = rows_aligned(table, table_ld, sizeof(T), 16) &&
+                         rows_aligned(out, out_ld, sizeof(T), 16) &&
+                         hidden % Row<T>::kCols == 0;
+    if (aligned)
+        embedding_rows_kernel<T, true><<<dim3((unsigned)blocks), dim3(256), 0, st>>>(
+            (const T*)table, vocab, hidden, table_ld, ids, n, scale, (T*)out, out_ld,
+            (int32_t)segs);
+    else
+        embedding_rows_kernel<T, false><<<dim3((unsigned)blocks), dim3(256), 0, st>>>(
+            (const T*)table, vocab, hidden, table_ld, ids, n, scale, (T*)out, out_ld,
+            (int32_t)segs);
+    return hipGetLastError();
+}
+
+// ---- sorting the ids -----------------------------------------------------------
+
+constexpr int kSortThreads = 512;
+constexpr int kSortWaves = kSortThreads / 64;
+constexpr int kMaxBins = 512;        // digits of at most 9 bits
+constexpr int kMaxSortBlocks = 256;
+
+struct SortPlan {
+    int32_t n, vocab;
+    int32_t per;       // items per block (a multiple of kSortThreads)
+    int32_t blocks;
+    int32_t bits;      // per digit
+    int32_t passes;
+};
+
+SortPlan sort_plan(int64_t n, int64_t vocab)
+{
+    SortPlan p;
+    p.n = (int32_t)n;
+    p.vocab = (int32_t)vocab;
+    int bits = 1;
+    while (((int64_t)1 << bits) <= vocab) ++bits;      // keys 0 .. vocab (padding)
+    p.passes = (bits + 8) / 9;
+    p.bits = (bits + p.passes - 1) / p.passes;
+    const int64_t per = round_up(div_up(n, kMaxSortBlocks), kSortThreads);
+    p.per = (int32_t)(per < 2 * kSortThreads ? 2 * kSortThreads : per);
+    p.blocks = (int32_t)div_up(n, p.per);
+    return p;
+}
+
+__device__ __forceinline__ int32_t key_of(const int64_t* ids, int32_t i, int32_t vocab)
+{
+    const int64_t id = ids[i];
+    return id >= 0 && id < vocab ? (int32_t)id : vocab;
+}
+
+// First digit's counts per block, and the clearing of what later kernels
+// count into: the other digits' counts and the flags of occurring tokens.
+__global__ __launch_bounds__(kSortThreads) void sort_count_kernel(SortPlan p, const int64_t* ids,
+                                                                  int32_t* hist, int32_t* later,
+                                                                  int64_t later_n,
+                                                                  uint32_t* flags,
+                                                                  int64_t flag_words)
+{
+    __shared__ int32_t s_hist[kMaxBins];
+    const int32_t bins = 1 << p.bits;
+    const int64_t at = (int64_t)blockIdx.x * kSortThreads + threadIdx.x;
+    const int64_t all = (int64_t)gridDim.x * kSortThreads;
+    for (int64_t i = at; i < later_n; i += all) later[i] = 0;
+    for (int64_t i = at; i < flag_words; i += all) flags[i] = 0;
+    if (blockIdx.x >= (unsigned)p.blocks) return;
+    for (int i = threadIdx.x; i < bins; i += kSortThreads) s_hist[i] = 0;
+    __syncthreads();
+    const int32_t begin = blockIdx.x * p.per;
+    const int32_t end = p.n - begin < p.per ? p.n : begin + p.per;
+    for (int32_t i = begin + threadIdx.x; i < end; i += kSortThreads)
+        atomicAdd(&s_hist[key_of(ids, i, p.vocab) & (bins - 1)], 1);
+    __syncthreads();
+    for (int i = threadIdx.x; i < bins; i += kSortThreads)
+        hist[blockIdx.x * bins + i] = s_hist[i];
+}
+
+// One stable pass by the digit at `shift`.  The first pass reads the ids,
+// later ones (key, position) pairs; each but the last counts the next digit
+// per destination block (integer atomics: the counts do not depend on their
+// order), the first also flags the tokens that occur.
+__global__ __launch_bounds__(kSortThreads) void sort_pass_kernel(SortPlan p, int32_t shift,
+                                                                 const int64_t* ids,
+                                                                 const int2* in,
+                                                                 const int32_t* hist,
+                                                                 int32_t* next_hist, int2* out,
+                                                                 uint8_t* flags)
+{
+    __shared__ int32_t s_base[kMaxBins];                // next output place per digit
+    __shared__ int32_t s_count[kSortWaves][kMaxBins];
+    __shared__ int32_t s_wave[kSortWaves];
+    const int32_t bins = 1 << p.bits;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+
+    // totals of each digit, and its counts in the blocks before this one
+    int32_t total = 0, before = 0;
+    if (tid < bins)
+        for (int32_t b = 0; b < p.blocks; ++b) {
+            const int32_t c = hist[b * bins + tid];
+            total += c;
+            before += b < (int32_t)blockIdx.x ? c : 0;
+        }
+    int32_t scan = total;                               // inclusive over the digits
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int32_t up = __shfl_up(scan, d);
+        if (lane >= d) scan += up;
+    }
+    if (lane == 63) s_wave[wave] = scan;
+    for (int w = 0; w < kSortWaves; ++w)
+        for (int i = tid; i < bins; i += kSortThreads) s_count[w][i] = 0;
+    __syncthreads();
+    int32_t base = scan - total + before;
+    for (int w = 0; w < wave; ++w) base += s_wave[w];
+    if (tid < bins) s_base[tid] = base;
+    __syncthreads();
+
+    const int32_t begin = blockIdx.x * p.per;
+    const int32_t end = p.n - begin < p.per ? p.n : begin + p.per;
+    for (int32_t first = begin; first < end; first += kSortThreads) {
+        const int32_t i = first + tid;
+        const bool live = i < end;
+        int2 item = make_int2(0, 0);
+        if (live) item = ids ? make_int2(key_of(ids, i, p.vocab), i) : in[i];
+        const int32_t d = (item.x >> shift) & (bins - 1);
+        // lanes of the wave with the same digit
+        uint64_t same = __ballot(live);
+        for (int b = 0; b < p.bits; ++b) {
+            const uint64_t set = __ballot((d >> b) & 1);
+            same &= (d >> b) & 1 ? set : ~set;
+        }
+        const int rank = __popcll(same & ((1ull << lane) - 1));
+        if (live && rank == 0) s_count[wave][d] = __popcll(same);
+        __syncthreads();
+        // exclusive over the waves, from the digit's next place
+        if (tid < bins) {
+            int32_t run = s_base[tid];
+#pragma unroll
+            for (int w = 0; w < kSortWaves; ++w) {
+                const int32_t c = s_count[w][tid];
+                s_count[w][tid] = run;
+                run += c;
+            }
+            s_base[tid] = run;
+        }
+        __syncthreads();
+        if (live) {
+            const int32_t to = s_count[wave][d] + rank;
+            out[to] = item;
+            if (next_hist)
+                atomicAdd(&next_hist[to / p.per * bins + ((item.x >> (shift + p.bits)) &
+                                                          (bins - 1))], 1);
+            if (flags && item.x < p.vocab) flags[item.x] = 1;
+        }
+        __syncthreads();
+        for (int w = 0; w < kSortWaves; ++w)
+            if (tid < bins) s_count[w][tid] = 0;
+        __syncthreads();
+    }
+}
+
+// ---- summing the sorted rows ---------------------------------------------------
+
+constexpr int kMaxChunk = 1024;
+
+struct SumArgs {
+    const int2* sorted;    // (token, position); padding (token == vocab) last
+    const void* grad;
+    void* out;
+    float* part;           // [chunks][2][pld]: the run that enters, the run that leaves
+    const uint8_t* flags;  // null: accumulate
+    int64_t grad_ld, out_ld, pld, hidden;
+    float scale;
+    int32_t n, vocab, chunk, chunks, zero_blocks, out_f32, accumulate;
+};
+
+template <int kCols, bool kAligned>
+struct Columns {
+    int64_t first, stride;
+    int64_t hidden;
+    __device__ __forceinline__ Columns(int64_t h)
+    {
+        const int64_t slab = (int64_t)blockIdx.y * blockDim.x * kCols;
+        first = kAligned ? slab + threadIdx.x * kCols : slab + threadIdx.x;
+        stride = kAligned ? 1 : blockDim.x;
+        hidden = h;
+    }
+    __device__ __forceinline__ int64_t col(int k) const { return first + k * stride; }
+    __device__ __forceinline__ bool has(int k) const { return col(k) < hidden; }
+};
+
+template <typename T, bool kAligned>
+__device__ __forceinline__ void load_row(const T* row, const Columns<Row<T>::kCols, kAligned>& c,
+                                         float (&x)[Row<T>::kCols])
+{
+    constexpr int kCols = Row<T>::kCols;
+    if constexpr (kAligned) {
+        typedef T vec __attribute__((ext_vector_type(kCols)));
+        const vec y = c.has(0) ? *(const vec*)(row + c.first) : vec(0);
+#pragma unroll
+        for (int k = 0; k < kCols; ++k) x[k] = Row<T>::value(y[k]);
+    } else {
+#pragma unroll
+        for (int k = 0; k < kCols; ++k) x[k] = c.has(k) ? Row<T>::value(row[c.col(k)]) : 0.f;
+    }
+}
+
+// A finished row of the table's gradient.
+template <int kCols, bool kAligned>
+__device__ __forceinline__ void store_row(const SumArgs& a, const Columns<kCols, kAligned>& c,
+                                          int64_t token, const float (&x)[kCols])
+{
+    if (a.out_f32) {
+        float* o = (float*)a.out + token * a.out_ld;
+        if constexpr (kAligned) {
+            if (!c.has(0)) return;
+#pragma unroll
+            for (int k = 0; k < kCols; k += 4) {
+                f32x4 y = f32x4{a.scale * x[k], a.scale * x[k + 1], a.scale * x[k + 2],
+                                a.scale * x[k + 3]};
+                f32x4* q = (f32x4*)(o + c.first + k);
+                if (a.accumulate) y += *q;
+                *q = y;
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < kCols; ++k)
+                if (c.has(k)) {
+                    float* q = o + c.col(k);
+                    *q = a.accumulate ? *q + a.scale * x[k] : a.scale * x[k];
+                }
+        }
+    } else {
+        uint16_t* o = (uint16_t*)a.out + token * a.out_ld;
+        if constexpr (kAligned) {
+            if (!c.has(0)) return;
+#pragma unroll
+            for (int k = 0; k < kCols; k += 4) {
+                uint16_t h[4];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) h[r] = to_bf16(a.scale * x[k + r]);
+                *(uint2*)(o + c.first + k) = make_uint2(h[0] | (uint32_t)h[1] << 16,
+                                                        h[2] | (uint32_t)h[3] << 16);
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < kCols; ++k)
+                if (c.has(k)) o[c.col(k)] = to_bf16(a.scale * x[k]);
+        }
+    }
+}
+
+template <int kCols, bool kAligned>
+__device__ __forceinline__ void store_part(const SumArgs& a, const Columns<kCols, kAligned>& c,
+                                           int64_t row, const float (&x)[kCols])
+{
+    float* o = a.part + row * a.pld;
+    if constexpr (kAligned) {
+        if (!c.has(0)) return;
+#pragma unroll
+        for (int k = 0; k < kCols; k += 4)
+            *(f32x4*)(o + c.first + k) = f32x4{x[k], x[k + 1], x[k + 2], x[k + 3]};
+    } else {
+#pragma unroll
+        for (int k = 0; k < kCols; ++k)
+            if (c.has(k)) o[c.col(k)] = x[k];
+    }
+}
+
+template <typename T, bool kAligned>
+__global__ __launch_bounds__(256) void embedding_sum_kernel(SumArgs a)
+{
+    constexpr int kCols = Row<T>::kCols;
+    __shared__ int2 s_item[kMaxChunk + 2];     // the entry before, the chunk, the entry after
+    const Columns<kCols, kAligned> c(a.hidden);
+    float zero[kCols];
+#pragma unroll
+    for (int k = 0; k < kCols; ++k) zero[k] = 0.f;
+    if (blockIdx.x >= (unsigned)a.chunks) {
+        // rows of tokens that do not occur
+        for (int64_t v = (int64_t)blockIdx.x - a.chunks; v < a.vocab; v += a.zero_blocks)
+            if (!a.flags[v]) store_row<kCols, kAligned>(a, c, v, zero);
+        return;
+    }
+    const int32_t begin = blockIdx.x * a.chunk;
+    const int32_t count = a.n - begin < a.chunk ? a.n - begin : a.chunk;
+    for (int32_t k = threadIdx.x; k < count + 2; k += blockDim.x) {
+        const int32_t i = begin + k - 1;
+        s_item[k] = i >= 0 && i < a.n ? a.sorted[i] : make_int2(a.vocab, 0);
+    }
+    __syncthreads();
+    const T* grad = (const T*)a.grad;
+    float acc[kCols];
+#pragma unroll
+    for (int k = 0; k < kCols; ++k) acc[k] = 0.f;
+    bool entered = s_item[0].x == s_item[1].x;
+    constexpr int kAhead = 4;
+    for (int32_t e0 = 0; e0 < count; e0 += kAhead) {
+        float x[kAhead][kCols];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const int2 it = s_item[1 + (e0 + u < count ? e0 + u : e0)];
+            if (it.x < a.vocab) load_row<T, kAligned>(grad + it.y * a.grad_ld, c, x[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            if (e0 + u >= count) break;
+            const int32_t token = __builtin_amdgcn_readfirstlane(s_item[1 + e0 + u].x);
+            if (token >= a.vocab) return;      // padding is last
+#pragma unroll
+            for (int k = 0; k < kCols; ++k) acc[k] += x[u][k];
+            const bool ends = s_item[2 + e0 + u].x != token;
+            if (ends || e0 + u + 1 == count) {
+                if (entered)
+                    store_part<kCols, kAligned>(a, c, 2 * (int64_t)blockIdx.x, acc);
+                else if (ends)
+                    store_row<kCols, kAligned>(a, c, token, acc);
+                else
+                    store_part<kCols, kAligned>(a, c, 2 * (int64_t)blockIdx.x + 1, acc);
+                entered = false;
+#pragma unroll
+                for (int k = 0; k < kCols; ++k) acc[k] = 0.f;
+            }
+        }
+    }
+}
+
+// Runs that cross chunk borders: the block of the chunk where a run begins
+// adds up its partials in order.
+template <int kCols, bool kAligned>
+__global__ __launch_bounds__(256) void embedding_join_kernel(SumArgs a)
+{
+    const int32_t ch = blockIdx.x;
+    const int32_t begin = ch * a.chunk, end = begin + a.chunk;
+    if (end >= a.n) return;                    // nothing leaves the last chunk
+    const int32_t token = a.sorted[end].x;
+    if (token >= a.vocab || a.sorted[end - 1].x != token) return;
+    if (a.sorted[begin].x == token && begin > 0 && a.sorted[begin - 1].x == token) return;
+    // chunks that the run reaches: chunk k continues it when its last entry
+    // and the one after have the token
+    const int lane = threadIdx.x & 63;
+    int32_t last = ch + 1;
+    for (;;) {
+        const int64_t next = ((int64_t)last + lane + 1) * a.chunk;
+        const bool on = next < a.n && a.sorted[next].x == token;
+        const uint64_t off = ~__ballot(on);
+        if (off) {
+            last += __builtin_ctzll(off);
+            break;
+        }
+        last += 64;
+    }
+    const Columns<kCols, kAligned> c(a.hidden);
+    float acc[kCols];
+    auto part = [&](int64_t row, float (&x)[kCols]) {
+        const float* p = a.part + row * a.pld;
+        if constexpr (kAligned) {
+#pragma unroll
+            for (int k = 0; k < kCols; k += 4) {
+                const f32x4 y = c.has(0) ? *(const f32x4*)(p + c.first + k) : f32x4(0.f);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) x[k + r] = y[r];
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < kCols; ++k) x[k] = c.has(k) ? p[c.col(k)] : 0.f;
+        }
+    };
+    part(2 * (int64_t)ch + 1, acc);
+    constexpr int kAhead = 4;
+    for (int32_t k0 = ch + 1; k0 <= last; k0 += kAhead) {
+        float x[kAhead][kCols];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) part(2 * (int64_t)(k0 + u <= last ? k0 + u : k0), x[u]);
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+            if (k0 + u <= last)
+#pragma unroll
+                for (int k = 0; k < kCols; ++k) acc[k] += x[u][k];
+    }
+    store_row<kCols, kAligned>(a, c, token, acc);
+}
+
+// Entries per chunk: 32 (the partial rows then cost at most a 16th of the
+// reads), more for long lists, so that neither the chunks nor the partials of
+// one run become very many.
+int32_t chunk_entries(int64_t n)
+{
+    const int64_t c = round_up(div_up(n, 2048), 32);
+    return (int32_t)(c < 32 ? 32 : c > kMaxChunk ? kMaxChunk : c);
+}
+
+struct GradBuffers {
+    int32_t* hist;         // [passes][blocks][bins]
+    int2* pairs[2];
+    uint32_t* flags;       // vocab bytes
+    float* part;
+};
+
+int64_t carve(int64_t n, int64_t vocab, int64_t hidden, void* ws, GradBuffers* b)
+{
+    const SortPlan p = sort_plan(n, vocab);
+    Carver c(ws);
+    b->hist = c.take<int32_t>((int64_t)p.passes * p.blocks << p.bits);
+    b->pairs[0] = c.take<int2>(n);
+    b->pairs[1] = c.take<int2>(p.passes > 1 ? n : 0);
+    b->flags = c.take<uint32_t>(div_up(vocab, 4));
+    b->part = c.take<float>(2 * div_up(n, chunk_entries(n)) * round_up(hidden, 8));
+    return c.used;
+}
+
+template <typename T>
+hipError_t launch_sum(const SumArgs& a, bool aligned, hipStream_t st)
+{
+    constexpr int kCols = Row<T>::kCols;
+    int64_t threads = round_up(div_up(a.hidden, kCols), 64);
+    if (threads > 256) threads = 256;
+    const dim3 block((unsigned)threads);
+    const unsigned slabs = (unsigned)div_up(a.hidden, threads * kCols);
+    const dim3 grid((unsigned)(a.chunks + a.zero_blocks), slabs), joins((unsigned)a.chunks, slabs);
+    if (aligned)
+        embedding_sum_kernel<T, true><<<grid, block, 0, st>>>(a);
+    else
+        embedding_sum_kernel<T, false><<<grid, block, 0, st>>>(a);
+    hipError_t err = hipGetLastError();
+    if (err != hipSuccess || a.chunks < 2) return err;
+    if (aligned)
+        embedding_join_kernel<kCols, true><<<joins, block, 0, st>>>(a);
+    else
+        embedding_join_kernel<kCols, false><<<joins, block, 0, st>>>(a);
+    return hipGetLastError();
+}
+
+hipError_t launch_grad(const void* grad, int32_t grad_type, int64_t grad_ld, const int64_t* ids,
+                       int64_t n, int64_t vocab, int64_t hidden, float scale, void* out,
+                       int32_t out_type, int64_t out_ld, bool accumulate, const GradBuffers& b,
+                       hipStream_t st)
+{
+    const SortPlan p = sort_plan(n, vocab);
+    const int64_t bins = (int64_t)1 << p.bits, per_pass = p.blocks * bins;
+    const int64_t words = accumulate ? 0 : div_up(vocab, 4);
+    const int64_t clear = (p.passes - 1) * per_pass + words;
+    int64_t blocks = div_up(clear, 4 * kSortThreads);
+    blocks = blocks < p.blocks ? p.blocks : blocks > 1024 ? 1024 : blocks;
+    sort_count_kernel<<<dim3((unsigned)blocks), dim3(kSortThreads), 0, st>>>(
+        p, ids, b.hist, b.hist + per_pass, (p.passes - 1) * per_pass, b.flags, words);
+    hipError_t err = hipGetLastError();
+    if (err != hipSuccess) return err;
+    for (int k = 0; k < p.passes; ++k) {
+        sort_pass_kernel<<<dim3((unsigned)p.blocks), dim3(kSortThreads), 0, st>>>(
+            p, k * p.bits, k == 0 ? ids : nullptr, k == 0 ? nullptr : b.pairs[(k + 1) & 1],
+            b.hist + k * per_pass, k + 1 < p.passes ? b.hist + (k + 1) * per_pass : nullptr,
+            b.pairs[k & 1], k == 0 && !accumulate ? (uint8_t*)b.flags : nullptr);
+        err = hipGetLastError();
+        if (err != hipSuccess) return err;
+    }
+    SumArgs a;
+    a.sorted = b.pairs[(p.passes - 1) & 1];
+    a.grad = grad;
+    a.out = out;
+    a.part = b.part;
+    a.flags = accumulate ? nullptr : (const uint8_t*)b.flags;
+    a.grad_ld = grad_ld;
+    a.out_ld = out_ld;
+    a.pld = round_up(hidden, 8);
+    a.hidden = hidden;
+    a.scale = scale;
+    a.n = (int32_t)n;
+    a.vocab = (int32_t)vocab;
+    a.chunk = chunk_entries(n);
+    a.chunks = (int32_t)div_up(n, a.chunk);
+    a.zero_blocks = accumulate ? 0 : (int32_t)(vocab < 2048 ? vocab : 2048);
+    a.out_f32 = out_type == DTE_TYPE_F32;
+    a.accumulate = accumulate;
+    const int64_t cols = grad_type == DTE_TYPE_F32 ? 4 : 8;
+    const bool aligned = hidden % cols == 0 &&
+                         rows_aligned(grad, grad_ld, type_size(grad_type), 16) &&
+                         rows_aligned(out, out_ld, type_size(out_type),
+                                      out_type == DTE_TYPE_F32 ? 16 : 8);
+    return grad_type == DTE_TYPE_F32 ? launch_sum<float>(a, aligned, st)
+                                     : launch_sum<uint16_t>(a, aligned, st);
+}
+
+// Every row of the table zero (no ids).
+__global__ __launch_bounds__(256) void zero_table_kernel(void* out, int64_t rows, int64_t cols,
+                                                         int64_t ld, int f32)
+{
+    const int64_t n = rows * cols;
+    for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < n;
+         q += (int64_t)gridDim.x * 256) {
+        const int64_t r = q / cols, c = q - r * cols;
+        if (f32)
+            ((float*)out)[r * ld + c] = 0.f;
+        else
+            ((uint16_t*)out)[r * ld + c] = 0;
+    }
+}
+
+constexpr int64_t kMaxCount = ((int64_t)1 << 31) - 65536;
+
+bool sizes_ok(int64_t n, int64_t vocab, int64_t hidden)
+{
+    return n >= 0 && n < kMaxCount && vocab >= 0 && vocab < kMaxCount && hidden >= 0 &&
+           hidden < kMaxLd;
+}
+
+}  // namespace
+}  // namespace dte
+
+extern "C" {
+
+dte_status dte_embedding_forward(const void* table, int32_t type, int64_t vocab, int64_t hidden,
+                                 int64_t table_ld, const int64_t* ids, int64_t n, float scale,
+                                 void* out, int64_t out_ld, void* stream)
+{
+    using namespace dte::tr;
+    if (!valid_type(type) || !std::isfinite(scale) || !dte::sizes_ok(n, vocab, hidden) ||
+        !valid_ld(table_ld, hidden) || !valid_ld(out_ld, hidden))
+        return DTE_ERR_ARG;
+    if (n == 0 || hidden == 0) return DTE_OK;
+    if ((!table && vocab > 0) || !ids || !out) return DTE_ERR_ARG;
+    hipStream_t st = (hipStream_t)stream;
+    const hipError_t err =
+        type == DTE_TYPE_F32
+            ? dte::launch_rows<float>(table, vocab, hidden, table_ld, ids, n, scale, out, out_ld,
+                                      st)
+            : dte::launch_rows<uint16_t>(table, vocab, hidden, table_ld, ids, n, scale, out,
+                                         out_ld, st);
+    return err == hipSuccess ? DTE_OK : DTE_ERR_HIP;
+}
+
+int64_t dte_embedding_workspace_bytes(int64_t n, int64_t vocab, int64_t hidden)
+{
+    if (!dte::sizes_ok(n, vocab, hidden)) return -1;
+    if (n == 0 || vocab == 0 || hidden == 0) return 0;
+    dte::GradBuffers b;
+    return dte::carve(n, vocab, hidden, nullptr, &b);
+}
+
+dte_status dte_embedding_backward(const void* grad, int32_t grad_type, int64_t grad_ld,
+                                  const int64_t* ids, int64_t n, int64_t vocab, int64_t hidden,
+                                  float scale, void* table_grad, int32_t table_type,
+                                  int64_t table_ld, int32_t accumulate, void* workspace,
+                                  int64_t workspace_bytes, void* stream)
+{
+    using namespace dte::tr;
+    if (!valid_type(grad_type) || !valid_type(table_type) || !std::isfinite(scale) ||
+        !dte::sizes_ok(n, vocab, hidden) || !valid_ld(grad_ld, hidden) ||
+        !valid_ld(table_ld, hidden))
+        return DTE_ERR_ARG;
+    if (accumulate && table_type != DTE_TYPE_F32) return DTE_ERR_ARG;
+    if (vocab == 0 || hidden == 0 || (n == 0 && accumulate)) return DTE_OK;
+    if (!table_grad) return DTE_ERR_ARG;
+    hipStream_t st = (hipStream_t)stream;
+    if (n == 0) {
+        dte::zero_table_kernel<<<dim3(4096), dim3(256), 0, st>>>(
+            table_grad, vocab, hidden, table_ld, table_type == DTE_TYPE_F32);
+        return hipGetLastError() == hipSuccess ? DTE_OK : DTE_ERR_HIP;
+    }
+    if (!grad || !ids) return DTE_ERR_ARG;
+    dte::GradBuffers b;
+    const int64_t need = dte::carve(n, vocab, hidden, workspace, &b);
+    if (!workspace_ok(workspace, workspace_bytes, need)) return DTE_ERR_ARG;
+    return dte::launch_grad(grad, grad_type, grad_ld, ids, n, vocab, hidden, scale, table_grad,
+                            table_type, table_ld, accumulate != 0, b, st) == hipSuccess
+               ? DTE_OK
+               : DTE_ERR_HIP;
+}
+
+}  // extern "C"

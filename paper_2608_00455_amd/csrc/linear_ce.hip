@@ -1,0 +1,696 @@
+// Linear cross entropy over a large vocabulary (include/dte_train.h):
+//
+//   z[t, v] = scale * h_t . w_v,  lse_t = log sum_v exp z[t, v]
+//   G[t, v] = scale * g_t * (exp(z[t, v] - lse_t) - [v == target_t])
+//   grad_h = G w,  grad_w = G^T h
+//
+// Forward: one pass of products over (vocabulary x tokens) tiles.  The
+// vocabulary is the i side, so a lane holds 4 FI logits of one token; their
+// maximum and sum of exponentials are taken in registers and joined across
+// lanes and waves, and a tile writes one (max, sum) pair per token.  A second
+// kernel joins the pairs.  No logit leaves the registers.
+//
+// Backward: piece by piece of the vocabulary, the logits again, G of the
+// piece in BF16 (workspace), and the two products with it.  grad_h is summed
+// over the pieces in binary32.  Recomputing the logits makes this 8 T V d
+// operations instead of 6 for the two directions together, and G of a piece
+// (rather than T x V logits) is all that is kept.
+//
+// Padding tokens: the hidden states are copied once to a padded array in
+// which padding rows are zero, so whatever they hold stays out of grad_w;
+// their rows of G are zero.
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+
+#include "abi_guard.h"
+#include "product.h"
+#include "train_common.h"
+
+namespace dte {
+namespace tr {
+
+int device_cus()
+{
+    static std::atomic<int> cache[64];
+    int dev = 0;
+    if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return 256;
+    int n = cache[dev].load(std::memory_order_relaxed);
+    if (n == 0) {
+        if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess ||
+            n <= 0)
+            n = 256;
+        cache[dev].store(n, std::memory_order_relaxed);
+    }
+    return n;
+}
+
+}  // namespace tr
+
+namespace {
+
+using namespace tr;
+using pr::f32x4;
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+__device__ __forceinline__ bool is_target(int64_t t, int64_t vocab) { return t >= 0 && t < vocab; }
+
+// ---- forward: (max, sum) per vocabulary tile and token ----------------------
+
+// Per token and vocabulary tile the maximum m of z (natural units) and the
+// sum of exp(z - m); z of the target where the tile holds it.
+struct StatsEpi {
+    struct Args {
+        const int64_t* targets;
+        float2* part;          // [tile rows][tpad]
+        float* target_z;       // [tpad]
+        int64_t tpad;
+        int32_t tokens;
+        int64_t vocab, v0;     // of the whole layer; first row of the operand
+        int32_t part0;         // first tile row of this launch
+        float scale;
+    };
+
+    template <class S>
+    static __device__ __forceinline__ void run(const Args& e, const pr::ProductArgs& p,
+                                               const pr::TileAt& at, const pr::LanePos<S>& pos,
+                                               f32x4 (&acc)[S::FI][S::FJ])
+    {
+        float2* s_pair = (float2*)pr::s_dynamic;     // [kWI][TJ]
+        const bool whole = pos.i - 4 * (pos.lane >> 4) + S::FI * 16 <= p.ni;
+        const int wi = pos.wave % S::kWI;
+#pragma unroll
+        for (int j = 0; j < S::FJ; ++j) {
+            const int64_t t = pos.j + 16 * j;
+            float m = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < S::FI; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    float z = acc[i][j][r] * e.scale;
+                    if (!whole && pos.i + 16 * i + r >= p.ni) z = -INFINITY;
+                    acc[i][j][r] = z;
+                    m = fmaxf(m, z);
+                }
+            // the target's logit, where this lane has it
+            if (t < e.tokens) {
+                const int64_t o = e.targets[t] - e.v0 - pos.i;
+                if (o >= 0 && o < S::FI * 16 && (o & 15) < 4) {
+#pragma unroll
+                    for (int i = 0; i < S::FI; ++i)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+                            if (o == 16 * i + r && pos.i + o < p.ni) e.target_z[t] = acc[i][j][r];
+                }
+            }
+            m = fmaxf(m, __shfl_xor(m, 16));
+            m = fmaxf(m, __shfl_xor(m, 32));
+            // a part that holds no vocabulary row at all adds nothing
+            const float top = m == -INFINITY ? 0.f : m;
+            float sum = 0.f;
+#pragma unroll
+            for (int i = 0; i < S::FI; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    sum += __builtin_amdgcn_exp2f((acc[i][j][r] - top) * kLog2e);
+            sum += __shfl_xor(sum, 16);
+            sum += __shfl_xor(sum, 32);
+            if ((pos.lane >> 4) == 0)
+                s_pair[wi * S::TJ + (int)(t - (int64_t)at.tj * S::TJ)] = make_float2(m, sum);
+        }
+        __syncthreads();
+        for (int x = threadIdx.x; x < S::TJ; x += S::kThreads) {
+            const int64_t t = (int64_t)at.tj * S::TJ + x;
+            if (t >= e.tpad) continue;
+            float2 a = s_pair[x];
+#pragma unroll
+            for (int w = 1; w < S::kWI; ++w) {
+                const float2 b = s_pair[w * S::TJ + x];
+                const float m = fmaxf(a.x, b.x);
+                const float o = m == -INFINITY ? 0.f : m;
+                a.y = a.y * __builtin_amdgcn_exp2f((a.x - o) * kLog2e) +
+                      b.y * __builtin_amdgcn_exp2f((b.x - o) * kLog2e);
+                a.x = m;
+            }
+            e.part[(int64_t)(e.part0 + at.ti) * e.tpad + t] = a;
+        }
+    }
+};
+
+// Joins the pairs of a token: 16 tokens per block, 16 lanes per token.
+__global__ __launch_bounds__(256) void join_stats_kernel(const float2* part, int64_t tpad,
+                                                         int32_t parts, const float* target_z,
+                                                         const int64_t* targets, int64_t vocab,
+                                                         int32_t tokens, float* loss, float* lse)
+{
+    __shared__ float2 s[16][17];
+    const int x = threadIdx.x & 15, y = threadIdx.x >> 4;
+    const int64_t t = (int64_t)blockIdx.x * 16 + x;
+    float m = -INFINITY, sum = 0.f;
+    if (t < tokens)
+        for (int32_t k = y; k < parts; k += 16) {
+            const float2 b = part[(int64_t)k * tpad + t];
+            const float n = fmaxf(m, b.x), o = n == -INFINITY ? 0.f : n;
+            sum = sum * __builtin_amdgcn_exp2f((m - o) * kLog2e) +
+                  b.y * __builtin_amdgcn_exp2f((b.x - o) * kLog2e);
+            m = n;
+        }
+    s[y][x] = make_float2(m, sum);
+    __syncthreads();
+    if (y != 0 || t >= tokens) return;
+    float top = s[0][x].x;
+    for (int k = 1; k < 16; ++k) top = fmaxf(top, s[k][x].x);
+    sum = 0.f;
+    for (int k = 0; k < 16; ++k)
+        if (s[k][x].x != -INFINITY || s[k][x].y != 0.f)
+            sum += s[k][x].y * __builtin_amdgcn_exp2f((s[k][x].x - top) * kLog2e);
+    const bool ok = is_target(targets[t], vocab);
+    const float l = top + __builtin_amdgcn_logf(sum) * kLn2;
+    lse[t] = ok ? l : 0.f;
+    loss[t] = ok ? l - target_z[t] : 0.f;
+}
+
+// ---- copies -----------------------------------------------------------------
+
+// dst[r, c] = src[r, c] for r < rows, c < cols, zero elsewhere in
+// [prows, pcols); rows whose target is padding are zero too.
+__global__ __launch_bounds__(256) void pad_rows_kernel(const uint16_t* src, int64_t ld,
+                                                       int64_t rows, int64_t cols,
+                                                       const int64_t* targets, int64_t vocab,
+                                                       uint16_t* dst, int64_t prows,
+                                                       int64_t pcols, int vec)
+{
+    const int64_t per = pcols / 8, n = prows * per;
+    for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < n;
+         q += (int64_t)gridDim.x * 256) {
+        const int64_t r = q / per, c = (q - r * per) * 8;
+        uint4 x = make_uint4(0, 0, 0, 0);
+        if (r < rows && c < cols && (!targets || is_target(targets[r], vocab))) {
+            const uint16_t* s = src + r * ld + c;
+            if (vec && c + 8 <= cols) {
+                x = *(const uint4*)s;
+            } else {
+                uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (c + k < cols) w[k >> 1] |= (uint32_t)s[k] << (16 * (k & 1));
+                x = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+        }
+        *(uint4*)(dst + r * pcols + c) = x;
+    }
+}
+
+hipError_t pad_rows(const uint16_t* src, int64_t ld, int64_t rows, int64_t cols,
+                    const int64_t* targets, int64_t vocab, uint16_t* dst, int64_t prows,
+                    int64_t pcols, hipStream_t stream)
+{
+    const int64_t blocks = div_up(prows * (pcols / 8), 256);
+    if (blocks == 0) return hipSuccess;
+    pad_rows_kernel<<<dim3((unsigned)(blocks < 4096 ? blocks : 4096)), dim3(256), 0, stream>>>(
+        src, ld, rows, cols, targets, vocab, dst, prows, pcols, rows_aligned(src, ld, 2, 16));
+    return hipGetLastError();
+}
+
+// ---- backward: G of a piece ---------------------------------------------------
+
+struct GradEpi {
+    struct Args {
+        const int64_t* targets;
+        const float* lse;
+        const float* grad_loss;
+        uint16_t* g;           // [terms][tpad][gld], columns of the piece
+        int64_t gld, term;     // row stride; elements between terms
+        int64_t tpad, v0, vocab;
+        int32_t tokens, terms;
+        float scale;
+    };
+
+    template <class S>
+    static __device__ __forceinline__ void run(const Args& e, const pr::ProductArgs& p,
+                                               const pr::TileAt& at, const pr::LanePos<S>& pos,
+                                               f32x4 (&acc)[S::FI][S::FJ])
+    {
+#pragma unroll
+        for (int j = 0; j < S::FJ; ++j) {
+            const int64_t t = pos.j + 16 * j;
+            if (t >= e.tpad) continue;
+            int64_t target = -1;
+            float lse = 0.f, w = 0.f;
+            bool ok = false;
+            if (t < e.tokens) {
+                target = e.targets[t];
+                ok = is_target(target, e.vocab);
+                lse = e.lse[t];
+                w = e.grad_loss[t] * e.scale;
+            }
+            const int64_t hot = target - e.v0 - pos.i;
+#pragma unroll
+            for (int i = 0; i < S::FI; ++i) {
+                if (pos.i + 16 * i >= e.gld) continue;
+                f32x4 g;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    // the difference is taken before the change of base: exact
+                    // to the rounding of the product
+                    float x = __builtin_amdgcn_exp2f(
+                        __builtin_fmaf(acc[i][j][r], e.scale, -lse) * kLog2e);
+                    if (hot == 16 * i + r) x -= 1.f;
+                    g[r] = ok && pos.i + 16 * i + r < p.ni ? x * w : 0.f;
+                }
+                uint16_t* dst = e.g + t * e.gld + pos.i + 16 * i;
+                for (int k = 0; k < e.terms; ++k) {
+                    uint16_t h[4];
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        h[r] = to_bf16(g[r]);
+                        g[r] -= from_bf16(h[r]);
+                    }
+                    *(uint2*)(dst + k * e.term) = make_uint2(h[0] | (uint32_t)h[1] << 16,
+                                                             h[2] | (uint32_t)h[3] << 16);
+                }
+            }
+        }
+    }
+};
+
+// ---- backward: the products with G --------------------------------------------
+
+// Binary32 sums [split][rows][ld], stored or added to.
+struct SumEpi {
+    struct Args {
+        float* out;
+        int64_t ld, part;      // elements between the splits' parts
+        int32_t add;
+    };
+    template <class S>
+    static __device__ __forceinline__ void run(const Args& e, const pr::ProductArgs& p,
+                                               const pr::TileAt& at, const pr::LanePos<S>& pos,
+                                               f32x4 (&acc)[S::FI][S::FJ])
+    {
+        float* out = e.out + at.split * e.part;
+#pragma unroll
+        for (int j = 0; j < S::FJ; ++j) {
+            const int64_t jj = pos.j + 16 * j;
+            if (jj >= p.nj) continue;
+#pragma unroll
+            for (int i = 0; i < S::FI; ++i) {
+                const int64_t ii = pos.i + 16 * i;
+                if (ii >= p.ni) continue;
+                f32x4* q = (f32x4*)(out + jj * e.ld + ii);
+                *q = e.add ? *q + acc[i][j] : acc[i][j];
+            }
+        }
+    }
+};
+
+// The user's weight gradient: any stride and alignment.
+struct WeightGradEpi {
+    struct Args {
+        void* out;
+        int64_t ld;
+        int32_t f32, add, vec;  // vec: rows 16-byte (F32) or 8-byte (BF16) aligned
+    };
+    template <class S>
+    static __device__ __forceinline__ void run(const Args& e, const pr::ProductArgs& p,
+                                               const pr::TileAt& at, const pr::LanePos<S>& pos,
+                                               f32x4 (&acc)[S::FI][S::FJ])
+    {
+#pragma unroll
+        for (int j = 0; j < S::FJ; ++j) {
+            const int64_t jj = pos.j + 16 * j;
+            if (jj >= p.nj) continue;
+#pragma unroll
+            for (int i = 0; i < S::FI; ++i) {
+                const int64_t ii = pos.i + 16 * i;
+                if (ii >= p.ni) continue;
+                const bool vec = e.vec && ii + 4 <= p.ni;
+                f32x4 x = acc[i][j];
+                if (e.f32) {
+                    float* q = (float*)e.out + jj * e.ld + ii;
+                    if (vec) {
+                        if (e.add) x += *(f32x4*)q;
+                        *(f32x4*)q = x;
+                    } else {
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+                            if (ii + r < p.ni) q[r] = e.add ? q[r] + x[r] : x[r];
+                    }
+                } else {
+                    uint16_t* q = (uint16_t*)e.out + jj * e.ld + ii;
+                    uint16_t h[4];
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) h[r] = to_bf16(x[r]);
+                    if (vec) {
+                        *(uint2*)q = make_uint2(h[0] | (uint32_t)h[1] << 16,
+                                                h[2] | (uint32_t)h[3] << 16);
+                    } else {
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+                            if (ii + r < p.ni) q[r] = h[r];
+                    }
+                }
+            }
+        }
+    }
+};
+
+// grad_hidden = BF16 of the splits' sums, in the splits' order.
+__global__ __launch_bounds__(256) void hidden_grad_kernel(const float* part, int64_t stride,
+                                                          int32_t splits, int64_t pld,
+                                                          int64_t rows, int64_t cols,
+                                                          uint16_t* out, int64_t ld, int vec)
+{
+    const int64_t per = (cols + 3) / 4, n = rows * per;
+    for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < n;
+         q += (int64_t)gridDim.x * 256) {
+        const int64_t r = q / per, c = (q - r * per) * 4;
+        f32x4 x = *(const f32x4*)(part + r * pld + c);
+        for (int32_t s = 1; s < splits; ++s)
+            x += *(const f32x4*)(part + s * stride + r * pld + c);
+        uint16_t h[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) h[k] = to_bf16(x[k]);
+        uint16_t* o = out + r * ld + c;
+        if (vec && c + 4 <= cols) {
+            *(uint2*)o = make_uint2(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (c + k < cols) o[k] = h[k];
+        }
+    }
+}
+
+// ---- the plan of a call ---------------------------------------------------------
+
+enum ShapeKind { kLarge, kMedium, kThin64, kThin32 };
+
+struct Sizes {
+    int64_t T, V, d, tpad, dpad;
+    bool pack;             // weight rows are copied to padded, aligned rows
+    int64_t piece;         // vocabulary rows per piece
+    int64_t gld;           // columns of G's rows
+    int32_t terms, split;
+    int64_t parts;         // tile rows of the forward statistics
+    ShapeKind logits, hid, wgt;
+};
+
+int tile_i(ShapeKind k) { return k == kMedium ? 128 : 256; }
+
+// Tile shape of a product with ni x nj outputs.  256 x 256 tiles read each
+// operand from LDS half as often as 128 x 128 ones, which is worth having once
+// there are tiles for most of the CUs; few j take the thin shapes, which do
+// not multiply rows that are not there.
+ShapeKind shape_for(int64_t ni, int64_t nj, int cus)
+{
+    if (nj <= 32) return kThin32;
+    if (nj <= 64) return kThin64;
+    const int64_t large = div_up(ni, 256) * div_up(nj, 256);
+    return large * 4 >= (int64_t)cus * 3 ? kLarge : kMedium;
+}
+
+constexpr int64_t kPieceBytes = (int64_t)256 << 20;   // of G
+
+bool sizes_of(const dte_linear_ce* c, bool backward, int32_t grad_type, Sizes* s)
+{
+    if (!c || c->reserved != 0 || !std::isfinite(c->scale)) return false;
+    if (c->tokens < 0 || c->vocab < 1 || c->dim < 1) return false;
+    if (c->tokens >= ((int64_t)1 << 31) - 512 || c->vocab >= ((int64_t)1 << 31) - 512 ||
+        c->dim >= 1 << 20)
+        return false;
+    if (!valid_ld(c->hidden_ld, c->dim) || !valid_ld(c->weight_ld, c->dim)) return false;
+    if (backward && !valid_type(grad_type)) return false;
+    const int cus = device_cus();
+    s->T = c->tokens;
+    s->V = c->vocab;
+    s->d = c->dim;
+    s->tpad = round_up(s->T, 64);
+    s->dpad = round_up(s->d, 64);
+    // the products load 16 bytes at 16-byte addresses and whole steps of 64
+    s->pack = s->d % 64 != 0 || !rows_aligned(c->weight, c->weight_ld, 2, 16);
+    s->logits = shape_for(s->V, s->T, cus);
+    s->terms = backward && grad_type == DTE_TYPE_F32 ? 3 : 1;
+    if (!backward) {
+        // the whole vocabulary at once, or what the packed copy has room for
+        s->piece = s->V;
+        if (s->pack) {
+            const int64_t rows = kPieceBytes / (s->dpad * 2) / 256 * 256;
+            s->piece = rows < 256 ? 256 : rows;
+            if (s->piece > s->V) s->piece = s->V;
+        }
+        s->parts = div_up(s->V, s->piece) * div_up(s->piece, tile_i(s->logits));
+        return true;
+    }
+    int64_t cols = s->tpad ? kPieceBytes / (s->tpad * 2 * s->terms) / 256 * 256 : 256;
+    if (cols < 4096) cols = 4096;
+    if (s->pack) {
+        int64_t most = kPieceBytes * 4 / (s->dpad * 2) / 256 * 256;
+        if (most < 4096) most = 4096;
+        if (cols > most) cols = most;
+    }
+    s->piece = cols < s->V ? cols : s->V;
+    s->gld = round_up(s->piece, 64);
+    s->hid = shape_for(s->d, s->T, cus);
+    s->wgt = shape_for(s->d, s->piece > 64 ? s->piece : 65, cus);
+    // few tiles of grad_hidden: share each tile's vocabulary rows among blocks
+    const int64_t ti = tile_i(s->hid);
+    const int64_t tj = s->hid == kLarge ? 256 : s->hid == kMedium ? 128 : s->hid == kThin64 ? 64 : 32;
+    const int64_t tiles = div_up(s->d, ti) * div_up(s->T > 0 ? s->T : 1, tj);
+    const int64_t slots = s->hid == kLarge ? cus : 2 * cus;
+    int64_t split = slots / tiles;
+    const int64_t most = div_up(s->piece, 64 * 4);   // at least four steps each
+    if (split > most) split = most;
+    s->split = (int32_t)(split < 1 ? 1 : split > 64 ? 64 : split);
+    return true;
+}
+
+struct Buffers {
+    uint16_t* h;           // [tpad][dpad]
+    uint16_t* w;           // [piece][dpad] (pack)
+    float2* part;          // forward
+    float* target_z;
+    uint16_t* g;           // backward: [terms][tpad][gld]
+    float* hsum;           // [split][tpad][dpad]
+};
+
+int64_t carve(const Sizes& s, bool backward, void* ws, Buffers* b)
+{
+    Carver c(ws);
+    b->h = c.take<uint16_t>(s.tpad * s.dpad);
+    b->w = s.pack ? c.take<uint16_t>(s.piece * s.dpad) : nullptr;
+    if (!backward) {
+        b->part = c.take<float2>(s.parts * s.tpad);
+        b->target_z = c.take<float>(s.tpad);
+    } else {
+        b->g = c.take<uint16_t>(s.terms * s.tpad * s.gld);
+        b->hsum = c.take<float>(s.split * s.tpad * s.dpad);
+    }
+    return c.used;
+}
+
+template <bool kAK, bool kBK, class Epi>
+hipError_t product(ShapeKind k, const pr::ProductArgs& p, const typename Epi::Args& e,
+                   hipStream_t st)
+{
+    switch (k) {
+    case kLarge: return pr::launch_product<pr::Large, false, kAK, kBK, Epi>(p, e, st);
+    case kMedium: return pr::launch_product<pr::Medium, false, kAK, kBK, Epi>(p, e, st);
+    default: break;
+    }
+    if constexpr (kBK) {      // the thin shapes take a k-contiguous j operand only
+        if (k == kThin64) return pr::launch_product<pr::Thin64, false, kAK, kBK, Epi>(p, e, st);
+        return pr::launch_product<pr::Thin32, false, kAK, kBK, Epi>(p, e, st);
+    }
+    return hipErrorInvalidValue;
+}
+
+pr::Operand operand(const uint16_t* p, int64_t ld, int64_t rows, int64_t kvalid, int32_t wrap = 0)
+{
+    return pr::Operand{p, ld, 0, (int32_t)rows, (int32_t)kvalid, wrap};
+}
+
+// Rows [v0, v0 + n) of the weight as an operand's memory.
+struct WeightRows {
+    const uint16_t* p;
+    int64_t ld;
+};
+
+hipError_t weight_rows(const dte_linear_ce* c, const Sizes& s, const Buffers& b, int64_t v0,
+                       int64_t n, hipStream_t st, WeightRows* w)
+{
+    const uint16_t* src = c->weight + v0 * c->weight_ld;
+    if (!s.pack) {
+        *w = WeightRows{src, c->weight_ld};
+        return hipSuccess;
+    }
+    *w = WeightRows{b.w, s.dpad};
+    return pad_rows(src, c->weight_ld, n, s.d, nullptr, 0, b.w, n, s.dpad, st);
+}
+
+pr::ProductArgs logits_product(const Sizes& s, const Buffers& b, const WeightRows& w, int64_t n)
+{
+    pr::ProductArgs p{};
+    p.a = operand(w.p, w.ld, n, 0);
+    p.b = operand(b.h, s.dpad, s.tpad, 0);
+    p.ni = (int32_t)n;
+    p.nj = (int32_t)s.tpad;
+    p.steps = (int32_t)(s.dpad / 64);
+    p.split = 1;
+    p.batch = 1;
+    return p;
+}
+
+#define DTE_TRY(x)                                 \
+    do {                                           \
+        if ((x) != hipSuccess) return DTE_ERR_HIP; \
+    } while (0)
+
+dte_status forward(const dte_linear_ce* c, const Sizes& s, const Buffers& b, float* loss,
+                   float* lse, hipStream_t st)
+{
+    DTE_TRY(pad_rows(c->hidden, c->hidden_ld, s.T, s.d, c->targets, s.V, b.h, s.tpad, s.dpad, st));
+    int32_t part0 = 0;
+    for (int64_t v0 = 0; v0 < s.V; v0 += s.piece) {
+        const int64_t n = s.V - v0 < s.piece ? s.V - v0 : s.piece;
+        WeightRows w;
+        DTE_TRY(weight_rows(c, s, b, v0, n, st, &w));
+        const pr::ProductArgs p = logits_product(s, b, w, n);
+        const StatsEpi::Args e{c->targets, b.part, b.target_z, s.tpad, (int32_t)s.T, s.V, v0,
+                               part0,      c->scale};
+        DTE_TRY((product<true, true, StatsEpi>(s.logits, p, e, st)));
+        part0 += (int32_t)div_up(n, tile_i(s.logits));
+    }
+    join_stats_kernel<<<dim3((unsigned)div_up(s.T, 16)), dim3(256), 0, st>>>(
+        b.part, s.tpad, part0, b.target_z, c->targets, s.V, (int32_t)s.T, loss, lse);
+    DTE_TRY(hipGetLastError());
+    return DTE_OK;
+}
+
+dte_status backward(const dte_linear_ce* c, const Sizes& s, const Buffers& b, const float* lse,
+                    const float* grad_loss, uint16_t* gh, int64_t gh_ld, void* gw, int32_t type,
+                    int64_t gw_ld, int32_t accumulate, hipStream_t st)
+{
+    const int64_t size = type_size(type);
+    DTE_TRY(pad_rows(c->hidden, c->hidden_ld, s.T, s.d, c->targets, s.V, b.h, s.tpad, s.dpad, st));
+    for (int64_t v0 = 0; v0 < s.V; v0 += s.piece) {
+        const int64_t n = s.V - v0 < s.piece ? s.V - v0 : s.piece;
+        WeightRows w;
+        DTE_TRY(weight_rows(c, s, b, v0, n, st, &w));
+        {
+            const pr::ProductArgs p = logits_product(s, b, w, n);
+            const GradEpi::Args e{c->targets, lse,  grad_loss, b.g,          s.gld,
+                                  s.tpad * s.gld, s.tpad, v0, s.V, (int32_t)s.T, s.terms,
+                                  c->scale};
+            DTE_TRY((product<true, true, GradEpi>(s.logits, p, e, st)));
+        }
+        if (gh) {
+            pr::ProductArgs p{};
+            p.a = operand(w.p, w.ld, s.pack ? s.dpad : s.d, n);
+            p.b = operand(b.g, s.gld, s.tpad, 0);
+            p.ni = (int32_t)s.dpad;
+            p.nj = (int32_t)s.tpad;
+            p.steps = (int32_t)div_up(n, 64);
+            p.split = s.split;
+            p.batch = 1;
+            const SumEpi::Args e{b.hsum, s.dpad, s.tpad * s.dpad, v0 > 0};
+            DTE_TRY((product<false, true, SumEpi>(s.hid, p, e, st)));
+        }
+        if (gw) {
+            pr::ProductArgs p{};
+            const int32_t tsteps = (int32_t)(s.tpad / 64);
+            p.a = operand(b.h, s.dpad, s.dpad, s.tpad, s.terms > 1 ? tsteps : 0);
+            p.b = operand(b.g, s.gld, s.gld, s.terms * s.tpad);
+            p.ni = (int32_t)s.d;
+            p.nj = (int32_t)n;
+            p.steps = tsteps * s.terms;
+            p.split = 1;
+            p.batch = 1;
+            void* out = (char*)gw + v0 * gw_ld * size;
+            const WeightGradEpi::Args e{out, gw_ld, type == DTE_TYPE_F32, accumulate != 0,
+                                        rows_aligned(gw, gw_ld, size, 4 * size)};
+            DTE_TRY((product<false, false, WeightGradEpi>(s.wgt, p, e, st)));
+        }
+    }
+    if (gh) {
+        const int64_t blocks = div_up(s.T * div_up(s.d, 4), 256);
+        hidden_grad_kernel<<<dim3((unsigned)(blocks < 8192 ? blocks : 8192)), dim3(256), 0, st>>>(
+            b.hsum, s.tpad * s.dpad, s.split, s.dpad, s.T, s.d, gh, gh_ld,
+            rows_aligned(gh, gh_ld, 2, 8));
+        DTE_TRY(hipGetLastError());
+    }
+    return DTE_OK;
+}
+
+// rows of zeros (no tokens: the weight's gradient is zero)
+__global__ void zero_rows_kernel(void* p, int64_t ld, int64_t rows, int64_t cols, int f32)
+{
+    const int64_t n = rows * cols;
+    for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < n;
+         q += (int64_t)gridDim.x * 256) {
+        const int64_t r = q / cols, c = q - r * cols;
+        if (f32)
+            ((float*)p)[r * ld + c] = 0.f;
+        else
+            ((uint16_t*)p)[r * ld + c] = 0;
+    }
+}
+
+}  // namespace
+}  // namespace dte
+
+extern "C" {
+
+int64_t dte_linear_ce_workspace_bytes(const dte_linear_ce* c, int32_t backward, int32_t grad_type)
+{
+    dte::Sizes s;
+    dte::Buffers b;
+    if (!dte::sizes_of(c, backward != 0, grad_type, &s)) return -1;
+    return dte::carve(s, backward != 0, nullptr, &b);
+}
+
+dte_status dte_linear_ce_forward(const dte_linear_ce* c, float* loss, float* lse, void* workspace,
+                                 int64_t workspace_bytes, void* stream)
+{
+    dte::Sizes s;
+    dte::Buffers b;
+    if (!dte::sizes_of(c, false, DTE_TYPE_F32, &s)) return DTE_ERR_ARG;
+    if (s.T == 0) return DTE_OK;
+    if (!c->hidden || !c->weight || !c->targets || !loss || !lse) return DTE_ERR_ARG;
+    const int64_t need = dte::carve(s, false, workspace, &b);
+    if (!dte::tr::workspace_ok(workspace, workspace_bytes, need)) return DTE_ERR_ARG;
+    return dte::no_throw([&] { return dte::forward(c, s, b, loss, lse, (hipStream_t)stream); });
+}
+
+dte_status dte_linear_ce_backward(const dte_linear_ce* c, const float* lse, const float* grad_loss,
+                                  uint16_t* grad_hidden, int64_t grad_hidden_ld,
+                                  void* grad_weight, int32_t grad_type, int64_t grad_weight_ld,
+                                  int32_t accumulate, void* workspace, int64_t workspace_bytes,
+                                  void* stream)
+{
+    dte::Sizes s;
+    dte::Buffers b;
+    if (!dte::sizes_of(c, true, grad_type, &s)) return DTE_ERR_ARG;
+    if (accumulate && grad_type != DTE_TYPE_F32) return DTE_ERR_ARG;
+    if (grad_hidden && !dte::tr::valid_ld(grad_hidden_ld, c->dim)) return DTE_ERR_ARG;
+    if (grad_weight && !dte::tr::valid_ld(grad_weight_ld, c->dim)) return DTE_ERR_ARG;
+    hipStream_t st = (hipStream_t)stream;
+    if (s.T == 0) {
+        if (!grad_weight || accumulate) return DTE_OK;
+        dte::zero_rows_kernel<<<dim3(4096), dim3(256), 0, st>>>(
+            grad_weight, grad_weight_ld, s.V, s.d, grad_type == DTE_TYPE_F32);
+        return hipGetLastError() == hipSuccess ? DTE_OK : DTE_ERR_HIP;
+    }
+    if (!grad_hidden && !grad_weight) return DTE_OK;
+    if (!c->hidden || !c->weight || !c->targets || !lse || !grad_loss) return DTE_ERR_ARG;
+    const int64_t need = dte::carve(s, true, workspace, &b);
+    if (!dte::tr::workspace_ok(workspace, workspace_bytes, need)) return DTE_ERR_ARG;
+    return dte::no_throw([&] {
+        return dte::backward(c, s, b, lse, grad_loss, grad_hidden, grad_hidden_ld, grad_weight,
+                             grad_type, grad_weight_ld, accumulate, st);
+    });
+}
+
+}  // extern "C"

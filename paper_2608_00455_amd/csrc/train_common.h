@@ -1,0 +1,59 @@
+// Shared by the trainer-side operators (include/dte_train.h): argument
+// checks, workspace layout, BF16 conversion and small device helpers.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "../../include/dte_train.h"
+
+namespace dte {
+namespace tr {
+
+constexpr int64_t kMaxLd = 1 << 22;
+
+inline bool valid_type(int32_t t) { return t == DTE_TYPE_F32 || t == DTE_TYPE_BF16; }
+inline int64_t type_size(int32_t t) { return t == DTE_TYPE_F32 ? 4 : 2; }
+inline bool valid_ld(int64_t ld, int64_t cols) { return ld >= cols && ld < kMaxLd; }
+__host__ __device__ inline int64_t round_up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
+__host__ __device__ inline int64_t div_up(int64_t x, int64_t m) { return (x + m - 1) / m; }
+
+// Rows that begin at `bytes`-aligned addresses.
+inline bool rows_aligned(const void* p, int64_t ld, int64_t elem, int64_t bytes)
+{
+    return (uintptr_t)p % bytes == 0 && ld * elem % bytes == 0;
+}
+
+// Parts of a workspace, each 256-byte aligned; with base 0 it only counts.
+struct Carver {
+    uintptr_t base;
+    int64_t used = 0;
+    explicit Carver(void* p) : base((uintptr_t)p) {}
+    template <typename T>
+    T* take(int64_t count)
+    {
+        T* q = (T*)(base + used);
+        used += round_up(count * (int64_t)sizeof(T), 256);
+        return q;
+    }
+};
+
+inline bool workspace_ok(const void* ws, int64_t bytes, int64_t need)
+{
+    return need == 0 || (ws && (uintptr_t)ws % 256 == 0 && bytes >= need);
+}
+
+int device_cus();
+
+// Round to nearest even (v_cvt_pk_bf16_f32).
+__device__ __forceinline__ uint16_t to_bf16(float x)
+{
+    return __builtin_bit_cast(uint16_t, (__bf16)x);
+}
+__device__ __forceinline__ float from_bf16(uint16_t x)
+{
+    return __builtin_bit_cast(float, (uint32_t)x << 16);
+}
+
+}  // namespace tr
+}  // namespace dte

@@ -1,0 +1,304 @@
+"""Trainer-side operators around the flat shard (include/dte_train.h): the
+vocabulary tables' lookup, loss and gradients, and the Muon step.
+
+torch is used for device memory and streams only; every operator runs inside
+libdte.so.  Tensors are checked here (type, shape, device, stride); matrices
+may have any row stride, with unit stride along a row.  Work is enqueued on
+`stream` (default: the current stream).  Outputs and workspaces are allocated
+with torch on that stream unless given; a workspace is a uint8 tensor of the
+library's size, 256-byte aligned, and may be given to save the allocation.
+Every function runs on the tensors' device.
+"""
+from __future__ import annotations
+
+import math
+from dataclasses import dataclass
+from typing import Sequence
+
+import torch
+
+from . import binding as B
+
+_TYPES = {torch.float32: B.DTE_TYPE_F32, torch.bfloat16: B.DTE_TYPE_BF16}
+
+# The Muon optimizer's quintic (published with it): five iterations take
+# singular values between about 0.01 and 1 to 0.7 .. 1.2.
+QUINTIC = (3.4445, -4.7750, 2.0315)
+
+
+def _type(t, name, types=_TYPES) -> int:
+    if not isinstance(t, torch.Tensor):
+        raise TypeError("%s: expected a torch.Tensor" % name)
+    if t.dtype not in types:
+        raise ValueError("%s: dtype %s, expected one of %s" % (
+            name, t.dtype, ", ".join(str(d) for d in types)))
+    return _TYPES.get(t.dtype, -1)
+
+
+def _array(t, dtype, shape, device, name):
+    """A dense tensor of the given type, shape and device."""
+    _type(t, name, (dtype,))
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError("%s: shape %s, expected %s" % (name, tuple(t.shape), tuple(shape)))
+    if t.device != device:
+        raise ValueError("%s: on %s, expected %s" % (name, t.device, device))
+    if not t.is_contiguous():
+        raise ValueError("%s: not contiguous" % name)
+
+
+def _ld(t, name) -> int:
+    """Row stride of a matrix (the last two dimensions) with unit stride along
+    a row."""
+    rows, cols = t.shape[-2], t.shape[-1]
+    if cols > 1 and t.stride(-1) != 1:
+        raise ValueError("%s: rows are not contiguous" % name)
+    if rows > 1 and t.stride(-2) < cols:
+        raise ValueError("%s: rows overlap" % name)
+    return t.stride(-2) if rows > 1 else max(1, cols)
+
+
+def _matrix(t, shape, device, name, types=_TYPES):
+    kind = _type(t, name, types)
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError("%s: shape %s, expected %s" % (name, tuple(t.shape), tuple(shape)))
+    if t.device != device:
+        raise ValueError("%s: on %s, expected %s" % (name, t.device, device))
+    return kind, _ld(t, name)
+
+
+class _On:
+    """The device of the call's tensors made current, and its stream."""
+
+    def __init__(self, device, stream):
+        if device.type != "cuda":
+            raise ValueError("tensors are on %s: a GPU is needed" % device)
+        self.device = device
+        self.stream = stream if stream is not None else torch.cuda.current_stream(device)
+        if self.stream.device != device:
+            raise ValueError("stream is on %s, the tensors on %s" % (self.stream.device, device))
+        self.context = torch.cuda.stream(self.stream)
+
+    def __enter__(self):
+        self.context.__enter__()
+        return self
+
+    def __exit__(self, *a):
+        return self.context.__exit__(*a)
+
+    @property
+    def handle(self) -> int:
+        return self.stream.cuda_stream
+
+    def empty(self, shape, dtype):
+        return torch.empty(shape, dtype=dtype, device=self.device)
+
+    def workspace(self, given, nbytes):
+        if nbytes < 0:
+            raise ValueError("sizes are out of the operator's range")
+        if given is None:
+            return self.empty(nbytes, torch.uint8)
+        _type(given, "workspace", (torch.uint8,))
+        if given.device != self.device or not given.is_contiguous():
+            raise ValueError("workspace: expected a dense tensor on %s" % self.device)
+        if given.numel() < nbytes or given.data_ptr() % 256:
+            raise ValueError("workspace: %d bytes at a 256-byte address needed" % nbytes)
+        return given
+
+
+# ---- embedding -----------------------------------------------------------------
+
+def embedding(table, ids, scale=1.0, out=None, stream=None):
+    """scale * table[ids]: table [vocab, hidden] float32 or bfloat16, ids
+    int64 [n]; the result has the table's type.  Ids outside the table are
+    padding (zero rows)."""
+    _type(table, "table")
+    if table.dim() != 2:
+        raise ValueError("table: expected a matrix")
+    if not isinstance(ids, torch.Tensor) or ids.dim() != 1:
+        raise ValueError("ids: expected a vector")
+    vocab, hidden = table.shape
+    n = ids.numel()
+    kind, ld = _matrix(table, (vocab, hidden), table.device, "table")
+    _array(ids, torch.int64, (n,), table.device, "ids")
+    with _On(table.device, stream) as on:
+        if out is None:
+            out = on.empty((n, hidden), table.dtype)
+        _, out_ld = _matrix(out, (n, hidden), table.device, "out", (table.dtype,))
+        B.dte_embedding_forward(table.data_ptr(), kind, vocab, hidden, ld, ids.data_ptr(), n,
+                                scale, out.data_ptr(), out_ld, on.handle)
+    return out
+
+
+def embedding_grad(grad, ids, table_grad, scale=1.0, accumulate=False, workspace=None,
+                   stream=None):
+    """Gradient of `embedding` by its table, into table_grad [vocab, hidden]
+    (every row, or added to it with accumulate=True, float32 only): grad [n,
+    hidden] and table_grad are float32 or bfloat16 each.  Returns
+    table_grad."""
+    _type(table_grad, "table_grad")
+    if table_grad.dim() != 2:
+        raise ValueError("table_grad: expected a matrix")
+    if not isinstance(ids, torch.Tensor) or ids.dim() != 1:
+        raise ValueError("ids: expected a vector")
+    vocab, hidden = table_grad.shape
+    n, device = ids.numel(), table_grad.device
+    tkind, tld = _matrix(table_grad, (vocab, hidden), device, "table_grad")
+    gkind, gld = _matrix(grad, (n, hidden), device, "grad")
+    _array(ids, torch.int64, (n,), device, "ids")
+    if accumulate and tkind != B.DTE_TYPE_F32:
+        raise ValueError("table_grad: accumulation needs float32")
+    with _On(device, stream) as on:
+        ws = on.workspace(workspace, B.dte_embedding_workspace_bytes(n, vocab, hidden))
+        B.dte_embedding_backward(grad.data_ptr(), gkind, gld, ids.data_ptr(), n, vocab, hidden,
+                                 scale, table_grad.data_ptr(), tkind, tld, int(accumulate),
+                                 ws.data_ptr(), ws.numel(), on.handle)
+    return table_grad
+
+
+# ---- linear cross entropy ---------------------------------------------------------
+
+def _linear_ce(hidden, weight, targets, scale):
+    for t, name in ((hidden, "hidden"), (weight, "weight")):
+        _type(t, name, (torch.bfloat16,))
+        if t.dim() != 2:
+            raise ValueError("%s: expected a matrix" % name)
+    tokens, dim = hidden.shape
+    vocab = weight.shape[0]
+    _, hld = _matrix(hidden, (tokens, dim), hidden.device, "hidden")
+    _, wld = _matrix(weight, (vocab, dim), hidden.device, "weight")
+    _array(targets, torch.int64, (tokens,), hidden.device, "targets")
+    return B.dte_linear_ce(hidden.data_ptr(), weight.data_ptr(), targets.data_ptr(), hld, wld,
+                           tokens, vocab, dim, scale, 0)
+
+
+def linear_ce(hidden, weight, targets, scale=1.0, workspace=None, stream=None):
+    """(loss, lse), float32 [tokens] each, of the logits scale * hidden @
+    weight.T (bfloat16 [tokens, dim] and [vocab, dim]) for int64 targets:
+    loss = -log softmax(logits)[target], lse = logsumexp(logits).  Targets
+    outside the vocabulary are padding (both 0)."""
+    c = _linear_ce(hidden, weight, targets, scale)
+    with _On(hidden.device, stream) as on:
+        ws = on.workspace(workspace, B.dte_linear_ce_workspace_bytes(c, 0))
+        loss, lse = on.empty((2, c.tokens), torch.float32)
+        B.dte_linear_ce_forward(c, loss.data_ptr(), lse.data_ptr(), ws.data_ptr(), ws.numel(),
+                                on.handle)
+    return loss, lse
+
+
+def linear_ce_grad(hidden, weight, targets, lse, grad_loss, grad_weight, grad_hidden=None,
+                   scale=1.0, accumulate=False, workspace=None, stream=None):
+    """Gradients of sum(grad_loss * loss) of `linear_ce` (grad_loss: float32
+    [tokens], the weight of each token's loss; lse: as `linear_ce` returned
+    it).  grad_weight [vocab, dim], bfloat16 or float32, is written (or added
+    to, float32 with accumulate=True); grad_hidden is bfloat16 [tokens, dim].
+    Returns (grad_hidden, grad_weight)."""
+    c = _linear_ce(hidden, weight, targets, scale)
+    device = hidden.device
+    _array(lse, torch.float32, (c.tokens,), device, "lse")
+    _array(grad_loss, torch.float32, (c.tokens,), device, "grad_loss")
+    kind, wld = _matrix(grad_weight, (c.vocab, c.dim), device, "grad_weight")
+    if accumulate and kind != B.DTE_TYPE_F32:
+        raise ValueError("grad_weight: accumulation needs float32")
+    with _On(device, stream) as on:
+        if grad_hidden is None:
+            grad_hidden = on.empty((c.tokens, c.dim), torch.bfloat16)
+        _, hld = _matrix(grad_hidden, (c.tokens, c.dim), device, "grad_hidden",
+                         (torch.bfloat16,))
+        ws = on.workspace(workspace, B.dte_linear_ce_workspace_bytes(c, 1, kind))
+        B.dte_linear_ce_backward(c, lse.data_ptr(), grad_loss.data_ptr(), grad_hidden.data_ptr(),
+                                 hld, grad_weight.data_ptr(), kind, wld, int(accumulate),
+                                 ws.data_ptr(), ws.numel(), on.handle)
+    return grad_hidden, grad_weight
+
+
+# ---- Newton-Schulz and Muon ---------------------------------------------------------
+
+def newton_schulz(steps=5, coefficients=QUINTIC, eps=1e-7) -> B.dte_newton_schulz:
+    """coefficients: (a, b, c) for every iteration, or one triple for each."""
+    triples = [coefficients] * steps if isinstance(coefficients[0], (int, float)) \
+        else list(coefficients)
+    if not 1 <= steps <= B.DTE_MAX_NS_STEPS or len(triples) != steps:
+        raise ValueError("coefficients: %d triples for %d steps (1 to %d)" % (
+            len(triples), steps, B.DTE_MAX_NS_STEPS))
+    ns = B.dte_newton_schulz(steps, 0, eps)
+    for k, t in enumerate(triples):
+        ns.coefficients[k][:] = [float(x) for x in t]
+    return ns
+
+
+def _batched(t, name):
+    if not isinstance(t, torch.Tensor):
+        raise TypeError("%s: expected a torch.Tensor" % name)
+    if t.dim() not in (2, 3):
+        raise ValueError("%s: expected a matrix or a batch of matrices" % name)
+    return (1,) * (3 - t.dim()) + tuple(t.shape)
+
+
+def orthogonalise(x, steps=5, coefficients=QUINTIC, eps=1e-7, out=None, workspace=None,
+                  stream=None):
+    """Newton-Schulz iterations on x [rows, cols] or [batch, rows, cols]
+    (float32 or bfloat16), each matrix by itself; bfloat16 result of x's
+    shape."""
+    batch, rows, cols = _batched(x, "x")
+    kind, ld = _matrix(x, x.shape, x.device, "x")
+    ns = newton_schulz(steps, coefficients, eps)
+    with _On(x.device, stream) as on:
+        if out is None:
+            out = on.empty(x.shape, torch.bfloat16)
+        _, out_ld = _matrix(out, x.shape, x.device, "out", (torch.bfloat16,))
+        stride = [t.stride(0) if t.dim() == 3 and batch > 1 else 0 for t in (x, out)]
+        ws = on.workspace(workspace, B.dte_orthogonalise_workspace_bytes(batch, rows, cols))
+        B.dte_orthogonalise(x.data_ptr(), kind, batch, rows, cols, ld, stride[0], ns,
+                            out.data_ptr(), out_ld, stride[1], ws.data_ptr(), ws.numel(),
+                            on.handle)
+    return out
+
+
+@dataclass(frozen=True)
+class MuonStep:
+    """Hyperparameters of a Muon step: p = (1 - lr*weight_decay) p - lr *
+    update_scale * O, O the orthogonalised momentum."""
+    lr: float
+    momentum: float = 0.95
+    nesterov: bool = True
+    weight_decay: float = 0.01
+    update_scale: float = 1.0
+    steps: int = 5
+    coefficients: Sequence = QUINTIC
+    eps: float = 1e-7
+
+    def c(self) -> B.dte_muon_step:
+        return B.dte_muon_step(self.lr, self.momentum, self.weight_decay, self.update_scale,
+                               int(self.nesterov), 0,
+                               newton_schulz(self.steps, self.coefficients, self.eps))
+
+    def inverse(self):
+        """The AdamW hyperparameters with which dte_extract_delta inverts this
+        step, given the update O as m (float32) and ones as v: beta1 = beta2 =
+        0 and eps = 0 make its u = rate * O."""
+        rate = self.lr * self.update_scale
+        if rate < 0.0:
+            raise ValueError("update_scale: the inverse needs a rate that is not negative")
+        wd = self.lr * self.weight_decay / rate if rate > 0.0 else 0.0
+        if rate == 0.0 and self.lr * self.weight_decay != 0.0:
+            raise ValueError("update_scale: weight decay without an update cannot be inverted")
+        return B.dte_adamw_step(rate, 0.0, 0.0, 0.0, wd, 1, B.DTE_ORDER_FOLDED, 0)
+
+
+def muon_forward(p, momentum, g, hp: MuonStep, update=None, workspace=None, stream=None):
+    """One Muon step in place on dense float32 p and momentum ([rows, cols] or
+    [batch, rows, cols]) with gradient g; returns the orthogonalised update
+    (bfloat16)."""
+    batch, rows, cols = _batched(p, "p")
+    for t, name in ((p, "p"), (momentum, "momentum"), (g, "g")):
+        _array(t, torch.float32, p.shape, p.device, name)
+    if not math.isfinite(hp.lr):
+        raise ValueError("lr: %r" % hp.lr)
+    with _On(p.device, stream) as on:
+        if update is None:
+            update = on.empty(p.shape, torch.bfloat16)
+        _array(update, torch.bfloat16, p.shape, p.device, "update")
+        ws = on.workspace(workspace, B.dte_orthogonalise_workspace_bytes(batch, rows, cols))
+        B.dte_muon_forward(p.data_ptr(), momentum.data_ptr(), g.data_ptr(), batch, rows, cols,
+                           hp.c(), update.data_ptr(), ws.data_ptr(), ws.numel(), on.handle)
+    return update
