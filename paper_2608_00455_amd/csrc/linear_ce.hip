@@ -222,6 +222,7 @@ struct GradEpi {
         const float* lse;
         const float* grad_loss;
         uint16_t* g;           // [terms][tpad][gld], columns of the piece
+        float* rest;           // [tpad]: what rounding took from the target's entry
         int64_t gld, term;     // row stride; elements between terms
         int64_t tpad, v0, vocab;
         int32_t tokens, terms;
@@ -260,6 +261,7 @@ struct GradEpi {
                     if (hot == 16 * i + r) x -= 1.f;
                     g[r] = ok && pos.i + 16 * i + r < p.ni ? x * w : 0.f;
                 }
+                const f32x4 whole = g;
                 uint16_t* dst = e.g + t * e.gld + pos.i + 16 * i;
                 for (int k = 0; k < e.terms; ++k) {
                     uint16_t h[4];
@@ -271,6 +273,10 @@ struct GradEpi {
                     *(uint2*)(dst + k * e.term) = make_uint2(h[0] | (uint32_t)h[1] << 16,
                                                              h[2] | (uint32_t)h[3] << 16);
                 }
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (ok && hot == 16 * i + r)
+                        e.rest[t] = whole[r] - from_bf16(to_bf16(whole[r]));
             }
         }
     }
@@ -357,11 +363,18 @@ struct WeightGradEpi {
     }
 };
 
-// grad_hidden = BF16 of the splits' sums, in the splits' order.
+// grad_hidden = BF16 of the splits' sums, in the splits' order, and of the
+// part of the target's entry of G that its rounding took away: that entry is
+// often most of a token's gradient, and its exact product costs one row of
+// the weight.
 __global__ __launch_bounds__(256) void hidden_grad_kernel(const float* part, int64_t stride,
                                                           int32_t splits, int64_t pld,
                                                           int64_t rows, int64_t cols,
-                                                          uint16_t* out, int64_t ld, int vec)
+                                                          const float* rest,
+                                                          const int64_t* targets, int64_t vocab,
+                                                          const uint16_t* weight,
+                                                          int64_t weight_ld, uint16_t* out,
+                                                          int64_t ld, int vec)
 {
     const int64_t per = (cols + 3) / 4, n = rows * per;
     for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < n;
@@ -370,6 +383,13 @@ __global__ __launch_bounds__(256) void hidden_grad_kernel(const float* part, int
         f32x4 x = *(const f32x4*)(part + r * pld + c);
         for (int32_t s = 1; s < splits; ++s)
             x += *(const f32x4*)(part + s * stride + r * pld + c);
+        const int64_t target = targets[r];
+        if (is_target(target, vocab)) {
+            const uint16_t* w = weight + target * weight_ld + c;
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (c + k < cols) x[k] += rest[r] * from_bf16(w[k]);
+        }
         uint16_t h[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) h[k] = to_bf16(x[k]);
@@ -474,6 +494,7 @@ struct Buffers {
     float* target_z;
     uint16_t* g;           // backward: [terms][tpad][gld]
     float* hsum;           // [split][tpad][dpad]
+    float* rest;           // [tpad]
 };
 
 int64_t carve(const Sizes& s, bool backward, void* ws, Buffers* b)
@@ -487,6 +508,7 @@ int64_t carve(const Sizes& s, bool backward, void* ws, Buffers* b)
     } else {
         b->g = c.take<uint16_t>(s.terms * s.tpad * s.gld);
         b->hsum = c.take<float>(s.split * s.tpad * s.dpad);
+        b->rest = c.take<float>(s.tpad);
     }
     return c.used;
 }
@@ -581,7 +603,7 @@ dte_status backward(const dte_linear_ce* c, const Sizes& s, const Buffers& b, co
         DTE_TRY(weight_rows(c, s, b, v0, n, st, &w));
         {
             const pr::ProductArgs p = logits_product(s, b, w, n);
-            const GradEpi::Args e{c->targets, lse,  grad_loss, b.g,          s.gld,
+            const GradEpi::Args e{c->targets, lse,  grad_loss, b.g, b.rest,       s.gld,
                                   s.tpad * s.gld, s.tpad, v0, s.V, (int32_t)s.T, s.terms,
                                   c->scale};
             DTE_TRY((product<true, true, GradEpi>(s.logits, p, e, st)));
@@ -617,7 +639,8 @@ dte_status backward(const dte_linear_ce* c, const Sizes& s, const Buffers& b, co
     if (gh) {
         const int64_t blocks = div_up(s.T * div_up(s.d, 4), 256);
         hidden_grad_kernel<<<dim3((unsigned)(blocks < 8192 ? blocks : 8192)), dim3(256), 0, st>>>(
-            b.hsum, s.tpad * s.dpad, s.split, s.dpad, s.T, s.d, gh, gh_ld,
+            b.hsum, s.tpad * s.dpad, s.split, s.dpad, s.T, s.d, b.rest, c->targets, s.V,
+            c->weight, c->weight_ld, gh, gh_ld,
             rows_aligned(gh, gh_ld, 2, 8));
         DTE_TRY(hipGetLastError());
     }

@@ -93,8 +93,7 @@ class _On:
         return torch.empty(shape, dtype=dtype, device=self.device)
 
     def workspace(self, given, nbytes):
-        if nbytes < 0:
-            raise ValueError("sizes are out of the operator's range")
+        nbytes = max(0, nbytes)   # negative: invalid arguments, which the call itself refuses
         if given is None:
             return self.empty(nbytes, torch.uint8)
         _type(given, "workspace", (torch.uint8,))

@@ -1,0 +1,639 @@
+"""The trainer-side operators (include/dte_train.h) against their definitions
+in 64 bits, at the sizes, strides and paddings where their kernels change
+path, with tolerances from the roundings that each result goes through.
+
+Unit roundoffs: binary32 2^-24, BF16 2^-8, FP16 2^-11.
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2608_00455_amd import binding as B
+from paper_2608_00455_amd import train
+
+pytestmark = pytest.mark.gpu
+
+U32, UBF = 2.0 ** -24, 2.0 ** -8
+CANARY = -7.0
+
+
+def say(*a):
+    print(*a, flush=True)
+
+
+def gen(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+def randn(g, *shape, scale=1.0, dtype=torch.float32):
+    return (scale * torch.randn(*shape, generator=g, device="cuda")).to(dtype)
+
+
+def placed(x, pad=0, offset=0, canary=CANARY):
+    """x as a view with row stride cols + pad at an element offset inside a
+    larger buffer of canaries: (view, buffer)."""
+    rows, cols = x.shape
+    buf = torch.full((offset + rows * (cols + pad) + 64,), canary, dtype=x.dtype, device="cuda")
+    view = buf[offset:offset + rows * (cols + pad)].view(rows, cols + pad)[:, :cols]
+    view.copy_(x)
+    return view, buf
+
+
+def untouched(view, buf):
+    """Whether everything of buf outside the view still is canary."""
+    mask = torch.ones(buf.numel(), dtype=torch.bool, device="cuda")
+    rows, cols = view.shape
+    start = view.storage_offset()
+    for_rows = torch.arange(rows, device="cuda")[:, None] * view.stride(0)
+    mask[(start + for_rows + torch.arange(cols, device="cuda")[None, :]).reshape(-1)] = False
+    return bool((buf[mask].float() == CANARY).all())
+
+
+def ids_for(g, n, vocab, padding=True):
+    """Token ids with one frequent token, ids outside the vocabulary on both
+    sides and the vocabulary's ends among them."""
+    ids = torch.randint(0, max(1, vocab), (n,), generator=g, device="cuda")
+    hot = torch.rand(n, generator=g, device="cuda") < 0.3
+    ids = torch.where(hot, torch.full_like(ids, vocab // 2), ids)
+    if n > 3:
+        ids[1], ids[2] = 0, vocab - 1
+    if padding and n > 6:
+        ids[3], ids[4], ids[5] = -1, vocab, 2 ** 40
+        ids[n // 2::7] = -100
+    return ids
+
+
+# ---- embedding -------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("vocab,hidden,n,pad,offset,scale", [
+    (1000, 256, 16, 0, 0, 1.0), (1000, 256, 0, 0, 0, 1.0), (7, 1, 5, 0, 0, 2.0),
+    (6002, 1001, 301, 0, 1, 31.6), (50, 4096, 33, 8, 8, 64.0), (50, 4100, 9, 4, 3, -0.5),
+    (300, 24, 1, 0, 0, 0.0), (3, 2056, 4097, 0, 0, 1.0),
+])
+def test_embedding_rows(dtype, vocab, hidden, n, pad, offset, scale):
+    say("case: embedding", dtype, vocab, hidden, n, pad, offset)
+    g = gen(n + hidden)
+    table, _ = placed(randn(g, vocab, hidden, dtype=dtype), pad, offset)
+    ids = ids_for(g, n, vocab)
+    out, buf = placed(torch.zeros(n, hidden, dtype=dtype, device="cuda"), pad, offset)
+    got = train.embedding(table, ids, scale=scale, out=out)
+    assert got is out
+    ok = (ids >= 0) & (ids < vocab)
+    want = (table[torch.where(ok, ids, 0)].float() * np.float32(scale)).to(dtype)
+    want[~ok] = 0
+    assert torch.equal(out, want)
+    assert untouched(out, buf)
+    assert torch.equal(train.embedding(table, ids, scale=scale), want)
+
+
+def check_embedding_grad(vocab, hidden, n, gdtype, tdtype, accumulate, pad=0, offset=0,
+                         scale=1.5, ids=None, seed=0):
+    g = gen(seed + n + hidden)
+    ids = ids_for(g, n, vocab) if ids is None else ids
+    grad, _ = placed(randn(g, n, hidden, dtype=gdtype), pad, offset)
+    old = randn(g, vocab, hidden) if accumulate else \
+        torch.full((vocab, hidden), float("nan"), dtype=tdtype, device="cuda")
+    out, buf = placed(old, pad, offset)
+    train.embedding_grad(grad, ids, out, scale=scale, accumulate=accumulate)
+    ok = ((ids >= 0) & (ids < vocab)).nonzero()[:, 0]
+    want = torch.zeros(vocab, hidden, dtype=torch.float64, device="cuda")
+    size = want.clone()
+    s = float(np.float32(scale))
+    want.index_add_(0, ids[ok], grad[ok].double() * s)
+    size.index_add_(0, ids[ok], grad[ok].double().abs() * abs(s))
+    count = torch.bincount(ids[ok], minlength=vocab)[:, None].double()
+    # count additions and one product in binary32
+    tol = (count + 2) * U32 * size
+    if accumulate:
+        want += old.double()
+        tol += U32 * want.abs()
+        assert torch.equal(out[count[:, 0] == 0], old[count[:, 0] == 0])
+    if tdtype == torch.bfloat16:
+        tol += UBF * want.abs()
+    err = (out.double() - want).abs()
+    assert not torch.isnan(out).any()
+    assert bool((err <= tol).all()), float((err - tol).max())
+    assert untouched(out, buf)
+    again, _ = placed(old, pad, offset)
+    train.embedding_grad(grad, ids, again, scale=scale, accumulate=accumulate)
+    assert torch.equal(out, again)
+
+
+@pytest.mark.parametrize("gdtype,tdtype,accumulate", [
+    (torch.float32, torch.float32, False), (torch.float32, torch.float32, True),
+    (torch.bfloat16, torch.float32, True), (torch.bfloat16, torch.bfloat16, False),
+])
+@pytest.mark.parametrize("vocab,hidden,n,pad,offset", [
+    (1, 8, 1, 0, 0), (1000, 256, 1, 0, 0), (40, 1, 33, 0, 0), (6002, 1001, 301, 0, 1),
+    (513, 72, 1024, 8, 8), (262145, 16, 1025, 0, 0), (5, 2048, 3001, 4, 2), (300000, 9, 70001, 0, 0),
+])
+def test_embedding_grad(gdtype, tdtype, accumulate, vocab, hidden, n, pad, offset):
+    say("case: embedding_grad", gdtype, tdtype, accumulate, vocab, hidden, n, pad, offset)
+    check_embedding_grad(vocab, hidden, n, gdtype, tdtype, accumulate, pad, offset)
+
+
+@pytest.mark.parametrize("n", [31, 32, 33, 64, 2500, 131072 + 17])
+def test_embedding_grad_of_one_token(n):
+    """Runs that fill chunks exactly, cross every border, and lie between
+    padding."""
+    say("case: embedding_grad one token", n)
+    ids = torch.full((n,), 3, dtype=torch.int64, device="cuda")
+    check_embedding_grad(7, 24, n, torch.float32, torch.float32, False, ids=ids)
+    ids[::5] = -1
+    check_embedding_grad(7, 24, n, torch.bfloat16, torch.float32, True, ids=ids)
+
+
+def test_embedding_grad_without_tokens():
+    out = torch.full((5, 12), 3.0, device="cuda")
+    none = torch.empty(0, dtype=torch.int64, device="cuda")
+    train.embedding_grad(torch.empty(0, 12, device="cuda"), none, out, accumulate=True)
+    assert bool((out == 3.0).all())
+    train.embedding_grad(torch.empty(0, 12, device="cuda"), none, out)
+    assert bool((out == 0.0).all())
+    ids = torch.full((40,), -1, dtype=torch.int64, device="cuda")
+    out.fill_(3.0)
+    train.embedding_grad(torch.full((40, 12), float("nan"), device="cuda"), ids, out)
+    assert bool((out == 0.0).all())
+
+
+# ---- linear cross entropy -----------------------------------------------------------
+
+class Exact:
+    """Loss and gradients in binary64, with bounds on what the operator's
+    roundings may do to each element."""
+
+    def __init__(self, h, w, target, gl, scale):
+        T, V, d = h.shape[0], w.shape[0], h.shape[1]
+        ok = (target >= 0) & (target < V)
+        h = torch.where(ok[:, None], h.double(), 0.0)
+        w, s = w.double(), float(np.float32(scale))
+        z = s * (h @ w.T.contiguous())
+        # a dot product of d terms in binary32, any order; the scale's product
+        zerr = (d + 2) * U32 * abs(s) * (h.abs() @ w.T.contiguous().abs()).amax(dim=1)
+        lse = torch.logsumexp(z, dim=1)
+        at = torch.where(ok, target, 0)[:, None]
+        zero = torch.zeros((), dtype=torch.float64, device="cuda")
+        self.lse = torch.where(ok, lse, zero)
+        self.loss = torch.where(ok, lse - z.gather(1, at)[:, 0], zero)
+        # V additions, exponentials and a logarithm of a few ulps, and the
+        # rounding of the sums that are as large as z
+        top = z.abs().amax(dim=1)
+        self.lse_tol = zerr + (V + 64) * U32 + 4 * U32 * (top + lse.abs())
+        self.loss_tol = self.lse_tol + zerr + 2 * U32 * (top + self.loss.abs())
+        if gl is None:
+            return
+        gl = torch.where(ok, gl.double(), zero)
+        p = torch.exp(z - lse[:, None])
+        G = p.scatter_add(1, at, torch.full_like(at, -1, dtype=torch.float64))
+        G *= (s * gl)[:, None]
+        self.dh, self.dw = G @ w, G.T.contiguous() @ h
+        # relative error of p: of z, lse and the exponential's argument
+        perr = (2 * zerr + self.lse_tol + 16 * U32 * (1 + top + lse.abs()))[:, None]
+        Gerr = p * perr * (s * gl).abs()[:, None] + 4 * U32 * G.abs()
+        aw, ah, T = w.abs(), h.abs(), max(T, 1)
+        self.dh_tol = (Gerr + (UBF + (V + 2) * U32) * G.abs()) @ aw + UBF * self.dh.abs() * 1.01
+        self.dw_tol = {
+            torch.bfloat16: (Gerr + (UBF + (T + 2) * U32) * G.abs()).T.contiguous() @ ah +
+            UBF * self.dw.abs() * 1.01,
+            torch.float32: (Gerr + (3 * T + 4) * U32 * G.abs()).T.contiguous() @ ah}
+
+
+def within(got, want, tol, what):
+    err = (got.double() - want).abs()
+    bad = ~(err <= tol + 1e-30)
+    assert not bool(bad.any()), (what, float(err[bad].max()) if bad.any() else 0,
+                                 int(bad.sum()), float((err / (tol + 1e-30)).nan_to_num(1e9).max()))
+
+
+def ce_inputs(seed, T, V, d, hpad=0, wpad=0, offset=0):
+    g = gen(seed)
+    w, _ = placed(randn(g, V, d, scale=0.3, dtype=torch.bfloat16), wpad, offset)
+    target = ids_for(g, T, V)
+    h = randn(g, T, d)
+    ok = (target >= 0) & (target < V)
+    # some tokens are confident about their target
+    lean = 6.0 * torch.rand(T, 1, generator=g, device="cuda") / (0.09 * d)
+    h = h + torch.where(ok[:, None], lean * w[torch.where(ok, target, 0)].float(), 0.0)
+    h[~ok] = float("nan")
+    if T > 8:
+        h[8][~ok[8]] = float("inf")
+    h, _ = placed(h.bfloat16(), hpad, offset)
+    gl = randn(g, T)
+    return h, w, target, gl
+
+
+CE_SIZES = [
+    # T, V, d, hidden pad, weight pad, offset
+    (1, 1, 1, 0, 0, 0), (1, 1000, 256, 0, 0, 0), (2, 257, 64, 0, 0, 0), (5, 31, 7, 0, 0, 0),
+    (33, 6002, 1001, 0, 0, 0), (16, 255, 128, 8, 8, 8), (64, 300, 192, 0, 0, 0),
+    (65, 513, 64, 3, 0, 0), (130, 1000, 200, 0, 0, 1), (300, 4099, 320, 0, 64, 0),
+    (257, 64, 65, 1, 1, 0), (520, 2048, 512, 0, 0, 0),
+]
+
+
+@pytest.mark.parametrize("scale", [1.0, -1.25])
+@pytest.mark.parametrize("T,V,d,hpad,wpad,offset", CE_SIZES)
+def test_linear_ce(T, V, d, hpad, wpad, offset, scale):
+    say("case: linear_ce", T, V, d, hpad, wpad, offset, scale)
+    h, w, target, gl = ce_inputs(T + V, T, V, d, hpad, wpad, offset)
+    ex = Exact(h, w, target, gl, scale)
+    loss, lse = train.linear_ce(h, w, target, scale=scale)
+    within(lse, ex.lse, ex.lse_tol, "lse")
+    within(loss, ex.loss, ex.loss_tol, "loss")
+    for dtype, acc in ((torch.bfloat16, False), (torch.float32, False), (torch.float32, True)):
+        old = randn(gen(1), V, d) if acc else torch.full((V, d), float("nan"), device="cuda",
+                                                         dtype=dtype)
+        gw, wbuf = placed(old, wpad, offset)
+        gh, hbuf = placed(torch.full((T, d), float("nan"), dtype=torch.bfloat16, device="cuda"),
+                          hpad, offset)
+        train.linear_ce_grad(h, w, target, lse, gl, gw, grad_hidden=gh, scale=scale,
+                             accumulate=acc)
+        within(gh, ex.dh, ex.dh_tol, "grad_hidden")
+        want, tol = ex.dw, ex.dw_tol[dtype]
+        if acc:
+            want = want + old.double()
+            tol = tol + U32 * 2 * want.abs()
+        within(gw, want, tol, "grad_weight %s %s" % (dtype, acc))
+        assert untouched(gw, wbuf) and untouched(gh, hbuf)
+        assert bool((gh[(target < 0) | (target >= V)] == 0).all())
+        gh2, gw2 = train.linear_ce_grad(h, w, target, lse, gl, placed(old, wpad, offset)[0],
+                                        scale=scale, accumulate=acc)
+        assert torch.equal(gh, gh2) and torch.equal(gw, gw2)
+
+
+def test_linear_ce_gradients_against_differences():
+    """The gradients along random directions against central differences of
+    the loss in binary64."""
+    T, V, d = 40, 700, 96
+    h, w, target, gl = ce_inputs(5, T, V, d)
+    ok = (target >= 0) & (target < V)
+    h = torch.where(ok[:, None], h, torch.zeros((), dtype=h.dtype, device="cuda")).contiguous()
+    loss, lse = train.linear_ce(h, w, target)
+    dh, dw = train.linear_ce_grad(h, w, target, lse, gl,
+                                  torch.empty(V, d, device="cuda"))
+
+    def objective(hh, ww):
+        z = hh @ ww.T.contiguous()
+        each = torch.logsumexp(z, 1) - z.gather(1, torch.where(ok, target, 0)[:, None])[:, 0]
+        return (torch.where(ok, each, 0.0) * gl.double()).sum()
+
+    h0, w0 = h.double(), w.double()
+    ex = Exact(h, w, target, gl, 1.0)
+    for k in range(4):
+        a, b = randn(gen(k), T, d).double(), randn(gen(100 + k), V, d).double()
+        eps = 1e-5
+        num = (objective(h0 + eps * a, w0 + eps * b) -
+               objective(h0 - eps * a, w0 - eps * b)) / (2 * eps)
+        got = (dh.double() * a).sum() + (dw.double() * b).sum()
+        tol = (ex.dh_tol * a.abs()).sum() + (ex.dw_tol[torch.float32] * b.abs()).sum() + 1e-6
+        assert abs(float(got - num)) <= float(tol), (float(got), float(num), float(tol))
+
+
+@pytest.mark.parametrize("T,V,d,dtype", [
+    (8192, 20003, 64, torch.bfloat16),     # pieces of the vocabulary
+    (4096, 12002, 72, torch.float32),      # three terms per piece, packed weight
+    (1000, 40000, 130, torch.bfloat16),
+])
+def test_linear_ce_pieces(T, V, d, dtype):
+    say("case: linear_ce pieces", T, V, d, dtype)
+    h, w, target, gl = ce_inputs(3, T, V, d)
+    ex = Exact(h, w, target, gl, 1.0)
+    loss, lse = train.linear_ce(h, w, target)
+    within(lse, ex.lse, ex.lse_tol, "lse")
+    within(loss, ex.loss, ex.loss_tol, "loss")
+    gh, gw = train.linear_ce_grad(h, w, target, lse, gl,
+                                  torch.empty(V, d, dtype=dtype, device="cuda"))
+    within(gh, ex.dh, ex.dh_tol, "grad_hidden")
+    within(gw, ex.dw, ex.dw_tol[dtype], "grad_weight")
+
+
+def test_linear_ce_packed_forward_in_pieces():
+    """More packed rows than one copy holds."""
+    T, V, d = 3, 1_100_007, 65
+    h, w, target, _ = ce_inputs(9, T, V, d)
+    target[0] = V - 1
+    h[0] = 0.25
+    ex = Exact(h, w, target, None, 1.0)
+    loss, lse = train.linear_ce(h, w, target)
+    within(lse, ex.lse, ex.lse_tol, "lse")
+    within(loss, ex.loss, ex.loss_tol, "loss")
+
+
+def test_linear_ce_only_padding_and_no_tokens():
+    V, d = 500, 96
+    w = randn(gen(0), V, d, dtype=torch.bfloat16)
+    for T in (0, 5, 70):
+        h = torch.full((T, d), float("nan"), dtype=torch.bfloat16, device="cuda")
+        target = torch.full((T,), -1, dtype=torch.int64, device="cuda")
+        gl = torch.full((T,), float("nan"), device="cuda")
+        loss, lse = train.linear_ce(h, w, target)
+        assert bool((loss == 0).all()) and bool((lse == 0).all())
+        for dtype, acc in ((torch.bfloat16, False), (torch.float32, True)):
+            gw = torch.full((V, d), 2.0, dtype=dtype, device="cuda")
+            gh, gw = train.linear_ce_grad(h, w, target, lse, gl, gw, accumulate=acc)
+            assert bool((gh == 0).all()) and bool((gw == (2.0 if acc else 0.0)).all())
+
+
+def test_linear_ce_extreme_logits():
+    """Logits of +-10^4: the maximum is taken out before exponentials."""
+    T, V, d = 70, 1000, 64
+    h, w, target, gl = ce_inputs(2, T, V, d)
+    ok = (target >= 0) & (target < V)
+    h = torch.where(ok[:, None], h * 64, h)
+    w = (w * 64).contiguous()
+    ex = Exact(h, w, target, gl, 4.0)
+    loss, lse = train.linear_ce(h, w, target, scale=4.0)
+    assert float(ex.lse.abs().max()) > 1e4
+    within(lse, ex.lse, ex.lse_tol, "lse")
+    within(loss, ex.loss, ex.loss_tol, "loss")
+
+
+def test_offsets_beyond_32_bits():
+    """Tables of more than 2^31 elements: the rows at their end."""
+    V, d = 540_000, 4096
+    w = torch.zeros(V, d, dtype=torch.bfloat16, device="cuda")
+    w[-300:] = randn(gen(1), 300, d, scale=0.05, dtype=torch.bfloat16)
+    ids = torch.tensor([V - 1, 5, V - 299, V - 1], device="cuda")
+    rows = train.embedding(w, ids, scale=2.0)
+    assert torch.equal(rows, (w[ids].float() * 2).bfloat16())
+    h = randn(gen(2), 4, d, dtype=torch.bfloat16)
+    gl = randn(gen(3), 4)
+    loss, lse = train.linear_ce(h, w, ids)
+    z = h.double() @ w[-300:].double().T.contiguous()
+    z = torch.cat([torch.zeros(4, V - 300, dtype=torch.float64, device="cuda"), z], 1)
+    want = torch.logsumexp(z, 1)
+    assert float((lse - want).abs().max()) < 1e-4
+    assert float((loss - (want - z.gather(1, ids[:, None])[:, 0])).abs().max()) < 2e-4
+    gw = torch.empty(V, d, dtype=torch.bfloat16, device="cuda")
+    gh, gw = train.linear_ce_grad(h, w, ids, lse, gl, gw)
+    G = torch.exp(z - want[:, None]).scatter_add(1, ids[:, None], -torch.ones(
+        4, 1, dtype=torch.float64, device="cuda")) * gl.double()[:, None]
+    for part in (slice(0, 300), slice(V - 300, V)):
+        exact = G[:, part].T.contiguous() @ h.double()
+        tol = 2.1 * UBF * (G[:, part].T.contiguous().abs() @ h.double().abs()) + 1e-12
+        within(gw[part], exact, tol, "grad_weight")
+    table = torch.empty(V, d, dtype=torch.bfloat16, device="cuda")
+    train.embedding_grad(h, ids, table)
+    assert bool((table[V - 1].float() - (h[0].float() + h[3].float())).abs().max() <
+                0.01 * h.float().abs().max())
+    assert torch.equal(table[V - 299], h[2]) and torch.equal(table[5], h[1])
+    assert bool((table[V - 2] == 0).all()) and bool((table[:5] == 0).all())
+
+
+# ---- Newton-Schulz and Muon ------------------------------------------------------------
+
+def exact_orth(x, triples, eps=1e-7):
+    y = x.double()
+    y = y / (y.norm() + eps)
+    for a, b, c in triples:
+        if y.shape[0] <= y.shape[1]:
+            s = y @ y.T.contiguous()
+            y = a * y + (b * s + c * s @ s) @ y
+        else:
+            s = y.T.contiguous() @ y
+            y = a * y + y @ (b * s + c * s @ s)
+    return y
+
+
+def momentum_like(g, batch, rows, cols, dtype=torch.float32, strong=4):
+    k = min(strong, rows, cols)
+    left, right = randn(g, batch, rows, k), randn(g, batch, k, cols)
+    x = torch.stack([left[b] @ right[b] for b in range(batch)])
+    return (1e-3 * (x + randn(g, batch, rows, cols))).to(dtype)
+
+
+# Five iterations, each rounding X, S (twice used) and B to FP16 (2^-11 at
+# most, a third of it in the mean), with amplifications of up to 2.8 (the
+# largest |b s^2 + c s^4|): under 1e-2 of the result in the 2-norm; then BF16.
+ORTH_TOL = 1e-2 + 2.0 ** -8
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("batch,rows,cols,pad,offset", [
+    (1, 1, 1, 0, 0), (1, 1, 70, 0, 0), (2, 65, 1, 0, 0), (1, 64, 64, 0, 0), (3, 100, 37, 1, 1),
+    (2, 127, 300, 4, 0), (1, 704, 256, 0, 0), (1, 257, 1001, 0, 3), (5, 130, 130, 0, 0),
+    (1, 1030, 515, 2, 0),
+])
+def test_orthogonalise(dtype, batch, rows, cols, pad, offset):
+    say("case: orthogonalise", dtype, batch, rows, cols, pad, offset)
+    x = momentum_like(gen(rows + cols), batch, rows, cols, dtype)
+    xv, _ = placed(x.reshape(batch * rows, cols), pad, offset)
+    xv = xv.unflatten(0, (batch, rows))
+    ov, buf = placed(torch.zeros(batch * rows, cols, dtype=torch.bfloat16, device="cuda"), pad,
+                     offset)
+    out = train.orthogonalise(xv, out=ov.unflatten(0, (batch, rows)))
+    for b in range(batch):
+        want = exact_orth(xv[b], [train.QUINTIC] * 5)
+        rel = float((out[b].double() - want).norm() / want.norm())
+        assert rel < ORTH_TOL, (b, rel)
+    assert untouched(ov, buf)
+    assert torch.equal(out, train.orthogonalise(xv))
+    if batch == 1:
+        assert torch.equal(out[0], train.orthogonalise(xv[0]))
+
+
+def test_orthogonalise_large_tiles():
+    x = momentum_like(gen(7), 1, 4096, 4160, strong=64)
+    out = train.orthogonalise(x)
+    want = exact_orth(x[0], [train.QUINTIC] * 5)
+    assert float((out[0].double() - want).norm() / want.norm()) < ORTH_TOL
+    x = momentum_like(gen(8), 40, 770, 500, strong=16)
+    out = train.orthogonalise(x)
+    for b in (0, 17, 39):
+        want = exact_orth(x[b], [train.QUINTIC] * 5)
+        assert float((out[b].double() - want).norm() / want.norm()) < ORTH_TOL
+
+
+def test_orthogonalise_scales_schedules_and_zeros():
+    g = gen(3)
+    x = momentum_like(g, 1, 90, 200)[0]
+    base = train.orthogonalise(x, eps=0.0)
+    # the result does not depend on the scale (powers of two: not in a bit),
+    # however far from one
+    for e in (-100, -40, 60, 100):
+        assert torch.equal(train.orthogonalise(torch.ldexp(x, torch.tensor(e, device="cuda")),
+                                               eps=0.0), base)
+    # a schedule of its own per iteration, and another number of iterations
+    sched = [(3.0, -3.2, 1.2), (2.0, -1.5, 0.5), (1.875, -1.25, 0.375)]
+    out = train.orthogonalise(x, steps=3, coefficients=sched)
+    want = exact_orth(x, sched)
+    assert float((out.double() - want).norm() / want.norm()) < ORTH_TOL
+    out = train.orthogonalise(x, steps=1, coefficients=(1.0, 0.0, 0.0))
+    assert float((out.double() - x.double() / x.double().norm()).norm()) < 2 * UBF
+    # zero matrices stay zero, beside others in a batch; one that is not finite
+    # does not touch its neighbours
+    b = torch.stack([torch.zeros_like(x), x, torch.full_like(x, float("nan")), x])
+    out = train.orthogonalise(b)
+    assert bool((out[0] == 0).all()) and torch.equal(out[1], out[3])
+    assert bool(torch.isnan(out[2]).all())
+    assert torch.equal(out[1], train.orthogonalise(x))
+    # matrices of a larger tensor: rows and matrices further apart
+    big = randn(g, 3, 100, 260)
+    view = big[:, :90, 10:210]
+    assert torch.equal(train.orthogonalise(view), train.orthogonalise(view.contiguous()))
+
+
+def test_orthogonalise_singular_values():
+    """Singular values between 0.01 and 1 of the norm end between 0.6 and
+    1.25: what the quintic is for."""
+    n = 96
+    q1, q2 = (torch.linalg.qr(randn(gen(k), n, n).double())[0] for k in (1, 2))
+    s = torch.logspace(-1.6, 0, n, dtype=torch.float64, device="cuda")
+    out = train.orthogonalise(((q1 * s) @ q2).float())
+    got = torch.linalg.svdvals(out.double().cpu())
+    assert 0.6 < float(got.min()) and float(got.max()) < 1.25
+
+
+@pytest.mark.parametrize("nesterov", [False, True])
+@pytest.mark.parametrize("batch,rows,cols", [(1, 64, 64), (3, 70, 33), (1, 256, 704), (2, 1, 5)])
+def test_muon_step_and_its_inverse(batch, rows, cols, nesterov):
+    say("case: muon", batch, rows, cols, nesterov)
+    g = gen(rows)
+    p0, m0 = randn(g, batch, rows, cols, scale=0.02), randn(g, batch, rows, cols, scale=1e-3)
+    grad = randn(g, batch, rows, cols, scale=1e-3)
+    hp = train.MuonStep(lr=1e-3, momentum=0.95, nesterov=nesterov, weight_decay=0.1,
+                        update_scale=0.2 * math.sqrt(max(rows, cols)))
+    p, m = p0.clone(), m0.clone()
+    o = train.muon_forward(p, m, grad, hp)
+    mu = np.float32(hp.momentum)
+    want_m = mu * m0.cpu().numpy() + grad.cpu().numpy()
+    assert np.array_equal(m.cpu().numpy(), want_m)
+    u = grad.cpu().numpy() + mu * want_m if nesterov else want_m
+    # the same update as orthogonalising the look-ahead by itself
+    u = torch.from_numpy(u).cuda()
+    assert torch.equal(o, train.orthogonalise(u))
+    of = o.float().cpu().numpy()
+    decay = np.float32(1.0 - hp.lr * hp.weight_decay)
+    rate = np.float32(hp.lr * hp.update_scale)
+    want_p = decay * p0.cpu().numpy() - rate * of
+    assert np.array_equal(p.cpu().numpy(), want_p)
+    # the inverse: previous weights from the current ones and the update
+    n = p.numel()
+    prev = torch.empty(n, device="cuda")
+    ones, of32 = torch.ones(n, device="cuda"), o.float().reshape(-1)
+    idx = torch.empty(n, dtype=torch.int64, device="cuda")
+    val = torch.empty(n, dtype=torch.int16, device="cuda")
+    cursor = torch.zeros(1, dtype=torch.int64, device="cuda")
+    B.dte_extract_delta(p.data_ptr(), of32.data_ptr(), ones.data_ptr(), n, 0, hp.inverse(),
+                        idx.data_ptr(), val.data_ptr(), n, cursor.data_ptr(), prev.data_ptr(),
+                        torch.cuda.current_stream().cuda_stream)
+    # the step's and the inverse's roundings: of decay*p and of the results
+    err = (prev.double() - p0.reshape(-1).double()).abs()
+    tol = 4 * U32 * (p0.reshape(-1).double().abs() + float(rate) * of32.double().abs())
+    assert bool((err <= tol).all())
+    changed = int(cursor.item())
+    assert 0 < changed <= n
+    got = dict(zip(idx[:changed].tolist(), val[:changed].tolist()))
+    new = p.reshape(-1).bfloat16().view(torch.int16)
+    assert all(int(new[i]) == v for i, v in list(got.items())[:200])
+
+
+# ---- streams, graphs, workspaces --------------------------------------------------------
+
+def test_other_streams_and_given_workspaces():
+    T, V, d = 70, 1000, 128
+    h, w, target, gl = ce_inputs(4, T, V, d)
+    loss, lse = train.linear_ce(h, w, target)
+    want = train.linear_ce_grad(h, w, target, lse, gl, torch.empty(V, d, device="cuda"))
+    x = momentum_like(gen(2), 1, 100, 64)[0]
+    o = train.orthogonalise(x)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    ws = torch.empty(64 << 20, dtype=torch.uint8, device="cuda")
+    loss2, lse2 = train.linear_ce(h, w, target, workspace=ws, stream=side)
+    got = train.linear_ce_grad(h, w, target, lse2, gl, torch.empty(V, d, device="cuda"),
+                               workspace=ws, stream=side)
+    o2 = train.orthogonalise(x, workspace=ws, stream=side)
+    side.synchronize()
+    assert torch.equal(loss, loss2) and torch.equal(lse, lse2) and torch.equal(o, o2)
+    assert torch.equal(want[0], got[0]) and torch.equal(want[1], got[1])
+
+
+def test_graph_replays_equal_eager_calls():
+    T, V, d = 40, 700, 96
+    ins = [ce_inputs(s, T, V, d) for s in (1, 2, 3)]
+    h, w, target, gl = (t.clone() for t in ins[0])
+    table = torch.empty(V, d, device="cuda")
+    gw = torch.empty(V, d, device="cuda")
+    ws = torch.empty(64 << 20, dtype=torch.uint8, device="cuda")
+    p, m = randn(gen(5), V, d), torch.zeros(V, d, device="cuda")
+    hp = train.MuonStep(lr=1e-3)
+
+    def step():
+        x = train.embedding(w, target, scale=2.0)
+        loss, lse = train.linear_ce(h, w, target, workspace=ws)
+        gh, _ = train.linear_ce_grad(h, w, target, lse, gl, gw, workspace=ws)
+        train.embedding_grad(gh, target, table, workspace=ws)
+        o = train.muon_forward(p, m, gw, hp, workspace=ws)
+        return x, loss, gh, o
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        outs = step()
+    for k in (1, 2, 0, 1):
+        for dst, src in zip((h, w, target, gl), ins[k]):
+            dst.copy_(src)
+        p.copy_(randn(gen(5), V, d))
+        m.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in (*outs, table, gw, p, m)]
+        p.copy_(randn(gen(5), V, d))
+        m.zero_()
+        want = [*step(), table, gw, p, m]
+        torch.cuda.synchronize()
+        for a, b in zip(got, want):
+            assert torch.equal(a, b)
+
+
+# ---- refusals -----------------------------------------------------------------------------
+
+def test_refusals():
+    f = dict(device="cuda")
+    table = torch.zeros(10, 8, **f)
+    ids = torch.zeros(4, dtype=torch.int64, **f)
+    h, w = torch.zeros(4, 8, dtype=torch.bfloat16, **f), torch.zeros(10, 8, dtype=torch.bfloat16, **f)
+    gl = torch.zeros(4, **f)
+    cases = [
+        lambda: train.embedding(table.half(), ids), lambda: train.embedding(table, ids.int()),
+        lambda: train.embedding(table.t(), ids), lambda: train.embedding(table.cpu(), ids),
+        lambda: train.embedding(table, ids.cpu()),
+        lambda: train.embedding(table, ids, out=torch.zeros(4, 7, **f)),
+        lambda: train.embedding(table, ids, out=torch.zeros(4, 8, dtype=torch.bfloat16, **f)),
+        lambda: train.embedding_grad(torch.zeros(3, 8, **f), ids, table),
+        lambda: train.embedding_grad(torch.zeros(4, 8, **f), ids, table.bfloat16(), accumulate=True),
+        lambda: train.embedding_grad(torch.zeros(4, 8, **f), ids, table,
+                                     workspace=torch.empty(8, dtype=torch.uint8, **f)),
+        lambda: train.linear_ce(h.float(), w, ids), lambda: train.linear_ce(h, w[:, :7], ids),
+        lambda: train.linear_ce(h, w, ids[:3]), lambda: train.linear_ce(h[0], w, ids),
+        lambda: train.linear_ce_grad(h, w, ids, gl, gl.double(), table),
+        lambda: train.linear_ce_grad(h, w, ids, gl, gl, table[:9]),
+        lambda: train.linear_ce_grad(h, w, ids, gl, gl, w.clone(), accumulate=True),
+        lambda: train.linear_ce_grad(h, w, ids, gl, gl, table, grad_hidden=torch.zeros(4, 8, **f)),
+        lambda: train.orthogonalise(table.double()), lambda: train.orthogonalise(table[0]),
+        lambda: train.orthogonalise(table, steps=0), lambda: train.orthogonalise(table, steps=17),
+        lambda: train.orthogonalise(table, out=table),
+        lambda: train.muon_forward(table, table[:9], table, train.MuonStep(lr=0.1)),
+        lambda: train.muon_forward(table, table.clone(), table.bfloat16(), train.MuonStep(lr=0.1)),
+    ]
+    for k, call in enumerate(cases):
+        with pytest.raises((ValueError, TypeError)):
+            call()
+            pytest.fail("case %d was accepted" % k)
+    for call in (lambda: train.embedding(table, ids, scale=float("nan")),
+                 lambda: train.linear_ce(h, w, ids, scale=float("inf")),
+                 lambda: train.orthogonalise(table, coefficients=(30.0, 0.0, 0.0)),
+                 lambda: train.orthogonalise(table, eps=-1.0),
+                 lambda: train.muon_forward(table, table.clone(), table.clone(),
+                                            train.MuonStep(lr=0.1, momentum=1.0)),
+                 lambda: train.muon_forward(table, table.clone(), table.clone(),
+                                            train.MuonStep(lr=2.0, weight_decay=1.0))):
+        with pytest.raises(B.DteError) as e:
+            call()
+        assert e.value.status == B.DTE_ERR_ARG
