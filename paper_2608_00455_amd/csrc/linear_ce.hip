@@ -513,18 +513,18 @@ int64_t carve(const Sizes& s, bool backward, void* ws, Buffers* b)
     return c.used;
 }
 
-template <bool kAK, bool kBK, class Epi>
+template <pr::Layout kA, pr::Layout kB, class Epi>
 hipError_t product(ShapeKind k, const pr::ProductArgs& p, const typename Epi::Args& e,
                    hipStream_t st)
 {
     switch (k) {
-    case kLarge: return pr::launch_product<pr::Large, false, kAK, kBK, Epi>(p, e, st);
-    case kMedium: return pr::launch_product<pr::Medium, false, kAK, kBK, Epi>(p, e, st);
+    case kLarge: return pr::launch_product<pr::Large, false, kA, kB, Epi>(p, e, st);
+    case kMedium: return pr::launch_product<pr::Medium, false, kA, kB, Epi>(p, e, st);
     default: break;
     }
-    if constexpr (kBK) {      // the thin shapes take a k-contiguous j operand only
-        if (k == kThin64) return pr::launch_product<pr::Thin64, false, kAK, kBK, Epi>(p, e, st);
-        return pr::launch_product<pr::Thin32, false, kAK, kBK, Epi>(p, e, st);
+    if constexpr (kB == pr::kK) {      // the thin shapes take a k-contiguous j operand only
+        if (k == kThin64) return pr::launch_product<pr::Thin64, false, kA, kB, Epi>(p, e, st);
+        return pr::launch_product<pr::Thin32, false, kA, kB, Epi>(p, e, st);
     }
     return hipErrorInvalidValue;
 }
@@ -582,7 +582,7 @@ dte_status forward(const dte_linear_ce* c, const Sizes& s, const Buffers& b, flo
         const pr::ProductArgs p = logits_product(s, b, w, n);
         const StatsEpi::Args e{c->targets, b.part, b.target_z, s.tpad, (int32_t)s.T, s.V, v0,
                                part0,      c->scale};
-        DTE_TRY((product<true, true, StatsEpi>(s.logits, p, e, st)));
+        DTE_TRY((product<pr::kK, pr::kK, StatsEpi>(s.logits, p, e, st)));
         part0 += (int32_t)div_up(n, tile_i(s.logits));
     }
     join_stats_kernel<<<dim3((unsigned)div_up(s.T, 16)), dim3(256), 0, st>>>(
@@ -606,7 +606,7 @@ dte_status backward(const dte_linear_ce* c, const Sizes& s, const Buffers& b, co
             const GradEpi::Args e{c->targets, lse,  grad_loss, b.g, b.rest,       s.gld,
                                   s.tpad * s.gld, s.tpad, v0, s.V, (int32_t)s.T, s.terms,
                                   c->scale};
-            DTE_TRY((product<true, true, GradEpi>(s.logits, p, e, st)));
+            DTE_TRY((product<pr::kK, pr::kK, GradEpi>(s.logits, p, e, st)));
         }
         if (gh) {
             pr::ProductArgs p{};
@@ -618,7 +618,7 @@ dte_status backward(const dte_linear_ce* c, const Sizes& s, const Buffers& b, co
             p.split = s.split;
             p.batch = 1;
             const SumEpi::Args e{b.hsum, s.dpad, s.tpad * s.dpad, v0 > 0};
-            DTE_TRY((product<false, true, SumEpi>(s.hid, p, e, st)));
+            DTE_TRY((product<pr::kRTail, pr::kK, SumEpi>(s.hid, p, e, st)));
         }
         if (gw) {
             pr::ProductArgs p{};
@@ -633,7 +633,7 @@ dte_status backward(const dte_linear_ce* c, const Sizes& s, const Buffers& b, co
             void* out = (char*)gw + v0 * gw_ld * size;
             const WeightGradEpi::Args e{out, gw_ld, type == DTE_TYPE_F32, accumulate != 0,
                                         rows_aligned(gw, gw_ld, size, 4 * size)};
-            DTE_TRY((product<false, false, WeightGradEpi>(s.wgt, p, e, st)));
+            DTE_TRY((product<pr::kR, pr::kR, WeightGradEpi>(s.wgt, p, e, st)));
         }
     }
     if (gh) {

@@ -409,12 +409,12 @@ bool large_tiles(int64_t ni, int64_t nj, int64_t batch, bool symmetric, int cus)
     return rounds(256, cus) * 4.0 <= rounds(128, 2 * cus) * 2.2;
 }
 
-template <bool kAK, bool kBK, class Epi>
+template <pr::Layout kA, pr::Layout kB, class Epi>
 hipError_t product(pr::ProductArgs p, const typename Epi::Args& e, hipStream_t st)
 {
     return large_tiles(p.ni, p.nj, p.batch, p.symmetric != 0, device_cus())
-               ? pr::launch_product<pr::Large, true, kAK, kBK, Epi>(p, e, st)
-               : pr::launch_product<pr::Medium, true, kAK, kBK, Epi>(p, e, st);
+               ? pr::launch_product<pr::Large, true, kA, kB, Epi>(p, e, st)
+               : pr::launch_product<pr::Medium, true, kA, kB, Epi>(p, e, st);
 }
 
 struct Muon {
@@ -460,15 +460,15 @@ hipError_t orthogonalise(const Source& src, const OrthSizes& z, const dte_newton
         p.batch = (int32_t)z.batch;
         p.symmetric = 1;
         const SquareEpi::Args es{b.s, nullptr, z.kpad, kk, (float)(ss / (xs * xs)), 0.f};
-        err = z.wide ? product<true, true, SquareEpi>(p, es, st)
-                     : product<false, false, SquareEpi>(p, es, st);
+        err = z.wide ? product<pr::kK, pr::kK, SquareEpi>(p, es, st)
+                     : product<pr::kR, pr::kR, SquareEpi>(p, es, st);
         if (err != hipSuccess) return err;
         // B = b S + c S S
         p.a = p.b = pr::Operand{b.s, z.kpad, kk, (int32_t)z.kpad, (int32_t)z.kpad, 0};
         p.steps = (int32_t)(z.kpad / 64);
         const SquareEpi::Args eb{b.b, b.s, z.kpad, kk, (float)(cc * bs / (ss * ss)),
                                  (float)(bc * bs / ss)};
-        err = product<true, true, SquareEpi>(p, eb, st);
+        err = product<pr::kK, pr::kK, SquareEpi>(p, eb, st);
         if (err != hipSuccess) return err;
         // X
         const bool last = k + 1 == ns.steps;
@@ -491,22 +491,22 @@ hipError_t orthogonalise(const Source& src, const OrthSizes& z, const dte_newton
         if (!last) {
             const NextEpi::Args e{b.x32, b.x16[(k + 1) & 1], z.cpad, n, (float)a, scale,
                                   (float)next};
-            err = z.wide ? product<false, true, NextEpi>(u, e, st)
-                         : product<true, true, NextEpi>(u, e, st);
+            err = z.wide ? product<pr::kR, pr::kK, NextEpi>(u, e, st)
+                         : product<pr::kK, pr::kK, NextEpi>(u, e, st);
         } else if (muon) {
             const LastEpi<true>::Args e{
                 b.x32, z.cpad, n, (float)a, scale, out, out_ld, out_stride, (int32_t)z.rows,
                 (int32_t)z.cols, rows_aligned(out, out_ld, 2, 8) && out_stride % 4 == 0,
                 rows_aligned(muon->p, z.cols, 4, 16), muon->p, muon->decay, muon->rate};
-            err = z.wide ? product<false, true, LastEpi<true>>(u, e, st)
-                         : product<true, true, LastEpi<true>>(u, e, st);
+            err = z.wide ? product<pr::kR, pr::kK, LastEpi<true>>(u, e, st)
+                         : product<pr::kK, pr::kK, LastEpi<true>>(u, e, st);
         } else {
             const LastEpi<false>::Args e{
                 b.x32, z.cpad, n, (float)a, scale, out, out_ld, out_stride, (int32_t)z.rows,
                 (int32_t)z.cols, rows_aligned(out, out_ld, 2, 8) && out_stride % 4 == 0, 0,
                 nullptr, 0.f, 0.f};
-            err = z.wide ? product<false, true, LastEpi<false>>(u, e, st)
-                         : product<true, true, LastEpi<false>>(u, e, st);
+            err = z.wide ? product<pr::kR, pr::kK, LastEpi<false>>(u, e, st)
+                         : product<pr::kK, pr::kK, LastEpi<false>>(u, e, st);
         }
         if (err != hipSuccess) return err;
         xs = next;

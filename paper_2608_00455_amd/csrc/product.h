@@ -9,12 +9,26 @@
 //
 // A block owns a tile of TI x TJ outputs and walks k in steps of 64.  Each
 // step's operand tiles go straight from memory to LDS (16-byte buffer loads
-// with an LDS destination), into the half of a double buffer that the waves
-// are not reading.  A wave's outputs stay in registers; it reads fragments
-// of 16 rows x 32 k and issues v_mfma_f32_16x16x32.  The i side is the
-// instruction's row operand, so a lane ends up with four consecutive i of one
-// j: 8- or 16-byte stores, and reductions over i that are nearly all within
-// a lane.
+// with an LDS destination), into one of two buffers.  A wave's outputs stay in
+// registers; it reads fragments of 16 rows x 32 k and issues
+// v_mfma_f32_16x16x32.  The i side is the instruction's row operand, so a lane
+// ends up with four consecutive i of one j: 8- or 16-byte stores, and
+// reductions over i that are nearly all within a lane.
+//
+// The loop is a pipeline with one barrier per step, at its middle: while the
+// first half (32 k) of step s is multiplied, the fragments of the second half
+// are read, after which nobody reads step s's buffer any more; the barrier
+// makes that known (and that step s + 1 has landed), and while the second half
+// is multiplied the loads of step s + 2 go into that buffer and the fragments
+// of step s + 1's first half are read.  Reads and loads are issued one row of
+// matrix instructions apart, or they would fill their queues and hold the
+// matrix instructions up.  8192^3 in BF16, TFLOP/s, k-contiguous operands /
+// one row-contiguous / both: 1160 / 1165 / 1155 (a library product with
+// k-contiguous operands: 1400); one barrier at the end of each step and no
+// interleaving: 1066 / 878 / 921; loads issued together after the barrier: 1112
+// / 1072 / 1045.  v_mfma_f32_32x32x16 in the same pipeline: 1090.  At 8192^3
+// the matrix cores are busy 74 % of the time, at a clock that the power limit
+// holds at 1.65 GHz.
 //
 // LDS images and bank conflicts (64 banks of 4 bytes, 16-byte chunks):
 //  - k-contiguous: row r is 128 bytes, chunk c (8 k) at position c ^ (r & 7);
@@ -41,17 +55,21 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kStepK = 64;              // k per step
 constexpr int64_t kMaxLd = 1 << 22;     // 256 rows of 2-byte elements stay within 32-bit offsets
 
+// How an operand lies in memory: k-contiguous, row-contiguous, or
+// row-contiguous with a number of k that need not be a multiple of 64 (the
+// last step then reads the last k again; the other operand holds zeros there).
+enum Layout { kK, kR, kRTail };
+
 // One operand.  rows: valid rows (tiles that reach past them read the last
-// one again); kvalid: valid k of a row-contiguous operand (steps that reach
-// past read the last one again: the other operand holds zeros there).  A
-// k-contiguous operand is readable, and zero on one side, up to the next
-// multiple of 64.  wrap > 0: after wrap steps the operand starts over at k = 0.
-// stride: elements between the matrices of a batch.
+// one again); kvalid: valid k (kRTail).  The other layouts are readable, and
+// zero on one side, up to the next multiple of 64 k.  wrap > 0: after wrap
+// steps the operand starts over at k = 0.  stride: elements between the
+// matrices of a batch.
 struct Operand {
     const uint16_t* p;
     int64_t ld;
@@ -102,8 +120,9 @@ __device__ __forceinline__ uint32_t lds_base()
 
 // Loads of one operand's tiles to LDS: TR rows x 64 k per step, kThreads
 // threads, kLoads 16-byte loads per thread.
-template <int TR, int kThreads, bool kKC>
+template <int TR, int kThreads, Layout kL>
 struct TileLoader {
+    static constexpr bool kKC = kL == kK;
     static constexpr int kLoads = TR * 8 / kThreads;
     static_assert(kLoads * kThreads == TR * 8, "whole loads");
     uint32_t off[kLoads];   // byte offset of each load from `base`
@@ -141,7 +160,7 @@ struct TileLoader {
         constexpr int kChunks = TR / 8;
         static_assert(kKC || kChunks >= 16, "the exclusive-or needs 16 chunks per row");
         const int last = (int)((o.rows - 1 - row0) >> 3);
-        const int klast = o.kvalid - 1 - s * kStepK;
+        const int klast = kL == kRTail ? o.kvalid - 1 - s * kStepK : kStepK;
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
             const int q = i * kThreads + tid, k = q / kChunks, pos = q % kChunks;
@@ -151,33 +170,42 @@ struct TileLoader {
         }
     }
 
-    // Step s into the LDS image at `lds`; afterwards base is at step s + 1.
-    __device__ __forceinline__ void issue(const Operand& o, int64_t row0, int32_t s, uint32_t lds,
-                                          int wave)
+    // Load i of the step that base is at, into the LDS image at `lds`.  Inline
+    // assembly, for the compiler would wait for every such load before each
+    // transposing LDS read; the loop below waits where it has to.
+    __device__ __forceinline__ void load(uint32_t lds, int wave, int i) const
     {
 #ifdef __HIP_DEVICE_COMPILE__
-        if constexpr (!kKC) {
-            if ((int64_t)(s + 1) * kStepK > o.kvalid && o.wrap == 0) offsets(o, row0, s);
-        }
-        __amdgpu_buffer_rsrc_t r =
-            __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, 0xffffffffu, 0x00020000);
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(
-                r, (DTE_LDS(void)*)(uintptr_t)(lds + i * kThreads * 16 + wave * 1024), 16, off[i],
-                0, 0, 0);
+        u32x4 r;
+        r.x = (uint32_t)base;
+        r.y = (uint32_t)(base >> 32) & 0xffffu;
+        r.z = 0xffffffffu;
+        r.w = 0x00020000u;
+        const uint32_t m = lds + i * kThreads * 16 + wave * 1024;
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(m),
+                     "v"(off[i]), "s"(r)
+                     : "memory");
+#endif
+    }
+
+    // To step s (the one after the last that was loaded).
+    __device__ __forceinline__ void advance(const Operand& o, int64_t row0, int32_t s)
+    {
         base += step;
         if (--left == 0) {
             base -= (int64_t)o.wrap * step;
             left = o.wrap;
         }
-#endif
+        if constexpr (kL == kRTail) {
+            if ((int64_t)(s + 1) * kStepK > o.kvalid) offsets(o, row0, s);
+        }
     }
 };
 
 // A wave's fragments of one operand: kFrags x 16 rows from row w0 of the tile.
-template <int TR, int kFrags, bool kKC>
+template <int TR, int kFrags, Layout kL>
 struct FragReader {
+    static constexpr bool kKC = kL == kK;
     uint32_t at[kKC ? 2 : kFrags];
 
     __device__ __forceinline__ void init(int w0)
@@ -265,12 +293,12 @@ typedef Shape<256, 64, 4, 1> Thin64;     // few j: the i operand streams past
 typedef Shape<256, 32, 4, 1> Thin32;
 
 // The k loop.  On return the block's waves have left the loop together and no
-// LDS load is in flight, so the epilogue may use all of the LDS.
-template <class S, bool kF16, bool kAK, bool kBK>
+// load to LDS is in flight, so the epilogue may use all of the LDS.
+template <class S, bool kF16, Layout kA, Layout kB>
 __device__ __forceinline__ void tile_product(const ProductArgs& p, const TileAt& at, int wave,
                                              f32x4 (&acc)[S::FI][S::FJ])
 {
-    constexpr uint32_t kStage = S::kStageBytes, kB = S::TI * kStepK * 2;
+    constexpr uint32_t kStage = S::kStageBytes, kBAt = S::TI * kStepK * 2;
     const int32_t per = (p.steps + p.split - 1) / p.split;
     const int32_t s0 = at.split * per, s1 = min(p.steps, s0 + per);
 #pragma unroll
@@ -280,46 +308,84 @@ __device__ __forceinline__ void tile_product(const ProductArgs& p, const TileAt&
     if (s0 >= s1) return;
 
     const int64_t i0 = (int64_t)at.ti * S::TI, j0 = (int64_t)at.tj * S::TJ;
-    TileLoader<S::TI, S::kThreads, kAK> la;
-    TileLoader<S::TJ, S::kThreads, kBK> lb;
+    TileLoader<S::TI, S::kThreads, kA> la;
+    TileLoader<S::TJ, S::kThreads, kB> lb;
     la.init(p.a, p.a.p + at.batch * p.a.stride, i0, s0);
     lb.init(p.b, p.b.p + at.batch * p.b.stride, j0, s0);
-    FragReader<S::TI, S::FI, kAK> fa;
-    FragReader<S::TJ, S::FJ, kBK> fb;
+    FragReader<S::TI, S::FI, kA> fa;
+    FragReader<S::TJ, S::FJ, kB> fb;
     fa.init(wave % S::kWI * S::FI * 16);
     fb.init(wave / S::kWI * S::FJ * 16);
 
+#ifdef __HIP_DEVICE_COMPILE__
     const uint32_t lds = lds_base();
-    la.issue(p.a, i0, s0, lds, wave);
-    lb.issue(p.b, j0, s0, lds + kB, wave);
+    constexpr int kLA = decltype(la)::kLoads, kLoads = kLA + decltype(lb)::kLoads;
+    constexpr int kPerRow = (kLoads + S::FI - 1) / S::FI;
+    static_assert(S::FJ <= S::FI, "a row of the loop reads at most one j fragment");
+    auto load = [&](uint32_t to, int i) {
+        if (i < kLA)
+            la.load(to, wave, i);
+        else if (i < kLoads)
+            lb.load(to + kBAt, wave, i - kLA);
+    };
+    auto advance = [&](int32_t s) {
+        la.advance(p.a, i0, s);
+        lb.advance(p.b, j0, s);
+    };
+    // steps s0 and s0 + 1 (the last one again where there is no more: what is
+    // loaded is then not used)
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) load(lds, i);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    if (s0 + 1 < s1) advance(s0 + 1);
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) load(lds + kStage, i);
+
+    s16x8 a[S::FI], b[2][S::FJ];
+#pragma unroll
+    for (int j = 0; j < S::FJ; ++j) b[0][j] = fb.read(lds + kBAt, j, 0);
+#pragma unroll
+    for (int i = 0; i < S::FI; ++i) a[i] = fa.read(lds, i, 0);
     for (int32_t s = s0; s < s1; ++s) {
         const uint32_t odd = (s - s0) & 1;
         const uint32_t cur = lds + (odd ? kStage : 0), next = lds + (odd ? 0 : kStage);
-        // this step's loads have landed for every wave, and every wave is
-        // done reading the other half
+        if (s + 2 < s1) advance(s + 2);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < S::FI; ++i) {
+            if (i < S::FJ) b[1][i] = fb.read(cur + kBAt, i, 1);
+            const s16x8 t = fa.read(cur, i, 1);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int j = 0; j < S::FJ; ++j) acc[i][j] = mfma<kF16>(a[i], b[0][j], acc[i][j]);
+            a[i] = t;
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        // step s + 1 has landed for every wave, and every wave is done reading
+        // step s's buffer
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        if (s + 1 < s1) {
-            la.issue(p.a, i0, s + 1, next, wave);
-            lb.issue(p.b, j0, s + 1, next + kB, wave);
-        }
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int kk = 0; kk < 2; ++kk) {
-            s16x8 a[S::FI], b[S::FJ];
+        for (int i = 0; i < S::FI; ++i) {
 #pragma unroll
-            for (int j = 0; j < S::FJ; ++j) b[j] = fb.read(cur + kB, j, kk);
+            for (int k = 0; k < kPerRow; ++k) load(cur, i * kPerRow + k);
+            if (i < S::FJ) b[0][i] = fb.read(next + kBAt, i, 0);
+            const s16x8 t = fa.read(next, i, 0);
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int i = 0; i < S::FI; ++i) a[i] = fa.read(cur, i, kk);
-#pragma unroll
-            for (int i = 0; i < S::FI; ++i)
-#pragma unroll
-                for (int j = 0; j < S::FJ; ++j) acc[i][j] = mfma<kF16>(a[i], b[j], acc[i][j]);
+            for (int j = 0; j < S::FJ; ++j) acc[i][j] = mfma<kF16>(a[i], b[1][j], acc[i][j]);
+            a[i] = t;
+            __builtin_amdgcn_sched_barrier(0);
         }
     }
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
+#endif
 }
 
 // Where a lane's outputs lie: acc[fi][fj][r] is
@@ -339,7 +405,7 @@ struct LanePos {
 };
 
 // Epi::run(args, product, at, pos, acc) takes the sums.
-template <class S, bool kF16, bool kAK, bool kBK, class Epi>
+template <class S, bool kF16, Layout kA, Layout kB, class Epi>
 __global__ __launch_bounds__(S::kThreads, 2) void product_kernel(ProductArgs p,
                                                                  typename Epi::Args e,
                                                                  int32_t per_matrix)
@@ -348,12 +414,12 @@ __global__ __launch_bounds__(S::kThreads, 2) void product_kernel(ProductArgs p,
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const TileAt at = tile_of(p, per_matrix);
     f32x4 acc[S::FI][S::FJ];
-    tile_product<S, kF16, kAK, kBK>(p, at, wave, acc);
+    tile_product<S, kF16, kA, kB>(p, at, wave, acc);
     Epi::template run<S>(e, p, at, LanePos<S>(at, wave), acc);
 #endif
 }
 
-template <class S, bool kF16, bool kAK, bool kBK, class Epi>
+template <class S, bool kF16, Layout kA, Layout kB, class Epi>
 hipError_t launch_product(ProductArgs p, const typename Epi::Args& e, hipStream_t stream)
 {
     p.tiles_i = (p.ni + S::TI - 1) / S::TI;
@@ -363,7 +429,7 @@ hipError_t launch_product(ProductArgs p, const typename Epi::Args& e, hipStream_
     const int64_t blocks = tiles * p.split * p.batch;
     if (blocks <= 0) return hipSuccess;
     if (blocks > 0x7fffffff) return hipErrorInvalidValue;
-    const void* k = (const void*)product_kernel<S, kF16, kAK, kBK, Epi>;
+    const void* k = (const void*)product_kernel<S, kF16, kA, kB, Epi>;
     if (S::kLds > 65536) {
         // more dynamic LDS than the default limit: an attribute of the
         // function, set once per device
@@ -378,7 +444,7 @@ hipError_t launch_product(ProductArgs p, const typename Epi::Args& e, hipStream_
             done.fetch_or(bit, std::memory_order_relaxed);
         }
     }
-    hipLaunchKernelGGL((product_kernel<S, kF16, kAK, kBK, Epi>), dim3((unsigned)blocks),
+    hipLaunchKernelGGL((product_kernel<S, kF16, kA, kB, Epi>), dim3((unsigned)blocks),
                        dim3(S::kThreads), S::kLds, stream, p, e, (int32_t)(tiles * p.split));
     return hipGetLastError();
 }
