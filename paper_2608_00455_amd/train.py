@@ -37,8 +37,9 @@ def _type(t, name, types=_TYPES) -> int:
 
 def _array(t, dtype, shape, device, name):
     """A dense tensor of the given type, shape and device."""
-    _type(t, name, (dtype,))
-    if tuple(t.shape) != tuple(shape):
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype:
+        _type(t, name, (dtype,))
+    if t.shape != shape:
         raise ValueError("%s: shape %s, expected %s" % (name, tuple(t.shape), tuple(shape)))
     if t.device != device:
         raise ValueError("%s: on %s, expected %s" % (name, t.device, device))
@@ -46,48 +47,54 @@ def _array(t, dtype, shape, device, name):
         raise ValueError("%s: not contiguous" % name)
 
 
-def _ld(t, name) -> int:
-    """Row stride of a matrix (the last two dimensions) with unit stride along
-    a row."""
-    rows, cols = t.shape[-2], t.shape[-1]
-    if cols > 1 and t.stride(-1) != 1:
-        raise ValueError("%s: rows are not contiguous" % name)
-    if rows > 1 and t.stride(-2) < cols:
-        raise ValueError("%s: rows overlap" % name)
-    return t.stride(-2) if rows > 1 else max(1, cols)
-
-
 def _matrix(t, shape, device, name, types=_TYPES):
+    """(type, row stride) of a matrix (the last two dimensions) with unit
+    stride along a row."""
     kind = _type(t, name, types)
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError("%s: shape %s, expected %s" % (name, tuple(t.shape), tuple(shape)))
     if t.device != device:
         raise ValueError("%s: on %s, expected %s" % (name, t.device, device))
-    return kind, _ld(t, name)
+    rows, cols = shape[-2:]
+    *_, ld, unit = t.stride()
+    if cols > 1 and unit != 1:
+        raise ValueError("%s: rows are not contiguous" % name)
+    if rows > 1 and ld < cols:
+        raise ValueError("%s: rows overlap" % name)
+    return kind, ld if rows > 1 else max(1, cols)
 
 
 class _On:
-    """The device of the call's tensors made current, and its stream."""
+    """The stream that a call enqueues on, current (with its device) while
+    outputs and workspaces are allocated.  On the current stream of the
+    current device, the usual case, nothing is switched: that costs more than
+    a small operator."""
+
+    __slots__ = ("device", "handle", "context")
 
     def __init__(self, device, stream):
         if device.type != "cuda":
             raise ValueError("tensors are on %s: a GPU is needed" % device)
         self.device = device
-        self.stream = stream if stream is not None else torch.cuda.current_stream(device)
-        if self.stream.device != device:
-            raise ValueError("stream is on %s, the tensors on %s" % (self.stream.device, device))
-        self.context = torch.cuda.stream(self.stream)
+        if stream is None and device.index == torch.cuda.current_device():
+            self.handle = torch._C._cuda_getCurrentRawStream(device.index)
+            self.context = None
+            return
+        if stream is None:
+            stream = torch.cuda.current_stream(device)
+        if stream.device != device:
+            raise ValueError("stream is on %s, the tensors on %s" % (stream.device, device))
+        self.handle = stream.cuda_stream
+        self.context = torch.cuda.stream(stream)
 
     def __enter__(self):
-        self.context.__enter__()
+        if self.context is not None:
+            self.context.__enter__()
         return self
 
     def __exit__(self, *a):
-        return self.context.__exit__(*a)
-
-    @property
-    def handle(self) -> int:
-        return self.stream.cuda_stream
+        if self.context is not None:
+            return self.context.__exit__(*a)
 
     def empty(self, shape, dtype):
         return torch.empty(shape, dtype=dtype, device=self.device)
@@ -116,13 +123,14 @@ def embedding(table, ids, scale=1.0, out=None, stream=None):
     if not isinstance(ids, torch.Tensor) or ids.dim() != 1:
         raise ValueError("ids: expected a vector")
     vocab, hidden = table.shape
-    n = ids.numel()
-    kind, ld = _matrix(table, (vocab, hidden), table.device, "table")
-    _array(ids, torch.int64, (n,), table.device, "ids")
-    with _On(table.device, stream) as on:
+    n, device = ids.numel(), table.device
+    kind, ld = _matrix(table, (vocab, hidden), device, "table")
+    _array(ids, torch.int64, (n,), device, "ids")
+    with _On(device, stream) as on:
         if out is None:
-            out = on.empty((n, hidden), table.dtype)
-        _, out_ld = _matrix(out, (n, hidden), table.device, "out", (table.dtype,))
+            out, out_ld = on.empty((n, hidden), table.dtype), max(1, hidden)
+        else:
+            _, out_ld = _matrix(out, (n, hidden), device, "out", (table.dtype,))
         B.dte_embedding_forward(table.data_ptr(), kind, vocab, hidden, ld, ids.data_ptr(), n,
                                 scale, out.data_ptr(), out_ld, on.handle)
     return out
