@@ -12,13 +12,15 @@
 // to a = 3.4, five of them by several hundred, so BF16 operands (8 bits) cost
 // percents of the result for matrices with a few strong directions.  Operands
 // are FP16 (11 bits) at the same matrix-core rate, scaled by the power of two
-// that the bound on the singular values allows, and the linear term a X is
-// taken from a binary32 copy of X, so a weak direction never passes through
-// the rounding of a strong one.  Relative error (2-norm, against binary64, 512
-// x 1024 and 1536^2, five quintic steps) of this scheme / FP16 without the
-// binary32 copy / BF16: random matrices 1.6e-3 / 1.3e-3 / 1.1e-2, 32 strong
-// directions over noise 2.2e-4 / 5.7e-3 / 4.6e-2, one strong direction 2e-4 /
-// 1.2e-1 / 9.7e-1.
+// that the bound on the singular values allows.  X is kept in two FP16 parts
+// (21 bits), of which the products use the upper and the linear term both, so
+// a weak direction never passes through the rounding of a strong one; and the
+// diagonal of B, its largest part near convergence, is kept apart in binary32
+// and joins the linear term.  Relative error (2-norm, against binary64, 512 x
+// 1024 and 1536^2, five quintic steps) of this scheme / with the diagonal in B /
+// with X in one part / in BF16: random matrices 7e-4 / 1.6e-3 / 1.3e-3 /
+// 1.1e-2, 32 strong directions over noise 2.5e-4 / 2.2e-4 / 5.7e-3 / 4.6e-2,
+// one strong direction 1.3e-4 / 1e-4 / 1.2e-1 / 9.7e-1.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -42,9 +44,19 @@ using pr::f32x4;
     return (float)__builtin_bit_cast(_Float16, x);
 }
 
-[[maybe_unused]] __device__ __forceinline__ uint32_t pack(uint16_t lo, uint16_t hi)
+[[maybe_unused]] __device__ __forceinline__ uint4 f16x8(const float* x)
 {
-    return lo | (uint32_t)hi << 16;
+    return make_uint4(pack(to_f16(x[0]), to_f16(x[1])), pack(to_f16(x[2]), to_f16(x[3])),
+                      pack(to_f16(x[4]), to_f16(x[5])), pack(to_f16(x[6]), to_f16(x[7])));
+}
+[[maybe_unused]] __device__ __forceinline__ void halves8(uint4 w, float (&x)[8])
+{
+    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        x[2 * k] = from_f16((uint16_t)u[k]);
+        x[2 * k + 1] = from_f16((uint16_t)(u[k] >> 16));
+    }
 }
 
 // ---- the matrix to work on -----------------------------------------------------
@@ -66,7 +78,7 @@ __device__ __forceinline__ float muon_value(const Source& s, float m, float g)
     return s.nesterov ? g + s.mu * m : m;
 }
 
-constexpr int kNormBlocks = 64;    // partial sums per matrix, at most
+constexpr int kMaxParts = 1024;    // partial sums per matrix, at most
 
 __device__ __forceinline__ double wave_sum(double x)
 {
@@ -75,233 +87,383 @@ __device__ __forceinline__ double wave_sum(double x)
     return x;
 }
 
+// Sum over a block of 256, in every thread; s: four doubles of LDS.
+__device__ __forceinline__ double block_sum(double x, double* s)
+{
+    x = wave_sum(x);
+    if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = x;
+    __syncthreads();
+    return (s[0] + s[1]) + (s[2] + s[3]);
+}
+
+// Four values of row r from column c; beyond the row zero.  kVec: rows begin
+// and end at 16-byte (binary32) or 8-byte (BF16) addresses.
+template <bool kVec>
+__device__ __forceinline__ f32x4 values(const Source& s, int64_t b, int32_t r, int32_t c,
+                                        int32_t rows, int32_t cols)
+{
+    f32x4 x = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (s.momentum) {
+        const int64_t at = (b * rows + r) * cols + c;
+        if constexpr (kVec) {
+            x = *(const f32x4*)(s.momentum + at);
+            if (s.nesterov) {
+                const f32x4 g = *(const f32x4*)(s.g + at);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) x[k] = muon_value(s, x[k], g[k]);
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (c + k < cols)
+                    x[k] = muon_value(s, s.momentum[at + k], s.nesterov ? s.g[at + k] : 0.f);
+        }
+        return x;
+    }
+    const int64_t at = b * s.stride + r * s.ld + c;
+    if (s.bf16) {
+        const uint16_t* q = (const uint16_t*)s.x + at;
+        if constexpr (kVec) {
+            const uint2 w = *(const uint2*)q;
+            x = f32x4{from_bf16((uint16_t)w.x), from_bf16((uint16_t)(w.x >> 16)),
+                      from_bf16((uint16_t)w.y), from_bf16((uint16_t)(w.y >> 16))};
+        } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (c + k < cols) x[k] = from_bf16(q[k]);
+        }
+    } else {
+        const float* q = (const float*)s.x + at;
+        if constexpr (kVec) {
+            x = *(const f32x4*)q;
+        } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (c + k < cols) x[k] = q[k];
+        }
+    }
+    return x;
+}
+
 // Partial sums of squares in binary64 (no overflow or underflow whatever the
 // matrix's scale); a Muon step's momentum is updated on the way.
+template <bool kVec>
 __global__ __launch_bounds__(256) void norm_kernel(Source s, int32_t rows, int32_t cols,
                                                    double* part)
 {
     __shared__ double s_sum[4];
     const int64_t b = blockIdx.y;
+    const uint32_t per = (uint32_t)(cols + 3) / 4, n = (uint32_t)rows * per;
     double sum = 0.0;
-    if (s.momentum) {
-        const int64_t n = (int64_t)rows * cols, per = div_up(n, (int64_t)gridDim.x);
-        const int64_t begin = blockIdx.x * per, end = begin + per < n ? begin + per : n;
-        float* m = s.momentum + b * n;
-        const float* g = s.g + b * n;
-        for (int64_t i = begin + threadIdx.x; i < end; i += 256) {
-            const float gi = g[i], mi = s.mu * m[i] + gi;
-            m[i] = mi;
-            const double u = muon_value(s, mi, gi);
-            sum += u * u;
-        }
-    } else {
-        for (int32_t r = blockIdx.x; r < rows; r += gridDim.x) {
-            const int64_t at = b * s.stride + r * s.ld;
-            for (int32_t c = threadIdx.x; c < cols; c += 256) {
-                const double u = s.bf16 ? from_bf16(((const uint16_t*)s.x)[at + c])
-                                        : ((const float*)s.x)[at + c];
-                sum += u * u;
+    for (uint32_t q = blockIdx.x * 256 + threadIdx.x; q < n; q += gridDim.x * 256) {
+        const int32_t r = (int32_t)(q / per), c = (int32_t)(q - r * per) * 4;
+        if (s.momentum) {
+            const int64_t at = (b * rows + r) * cols + c;
+            if constexpr (kVec) {
+                const f32x4 m = *(const f32x4*)(s.momentum + at) * s.mu +
+                                *(const f32x4*)(s.g + at);
+                *(f32x4*)(s.momentum + at) = m;
+            } else {
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (c + k < cols)
+                        s.momentum[at + k] = s.mu * s.momentum[at + k] + s.g[at + k];
             }
         }
+        const f32x4 u = values<kVec>(s, b, r, c, rows, cols);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) sum += (double)u[k] * u[k];
     }
-    sum = wave_sum(sum);
-    if ((threadIdx.x & 63) == 0) s_sum[threadIdx.x >> 6] = sum;
-    __syncthreads();
-    if (threadIdx.x == 0)
-        part[b * gridDim.x + blockIdx.x] = (s_sum[0] + s_sum[1]) + (s_sum[2] + s_sum[3]);
+    sum = block_sum(sum, s_sum);
+    if (threadIdx.x == 0) part[b * gridDim.x + blockIdx.x] = sum;
 }
 
-// X_0 = x / (|x| + eps), padded with zeros to [rpad, cpad], in binary32 and in
-// scaled FP16.
-__global__ __launch_bounds__(256) void normalise_kernel(Source s, int32_t rows, int32_t cols,
-                                                        int64_t rpad, int64_t cpad,
-                                                        const double* part, int32_t parts,
-                                                        double eps, float scale, float* x32,
-                                                        uint16_t* x16)
+// X in two FP16 parts: hi the scaled value, lo 1024 times what is left.
+constexpr float kLoScale = 1024.f;
+
+struct Split4 {
+    uint2 hi, lo;
+};
+__device__ __forceinline__ Split4 split(f32x4 x)
 {
-    __shared__ float s_inv;
-    const int64_t b = blockIdx.y;
-    if (threadIdx.x < 64) {
-        double sum = threadIdx.x < (unsigned)parts ? part[b * parts + threadIdx.x] : 0.0;
-        sum = wave_sum(sum);
-        if (threadIdx.x == 0) s_inv = (float)(1.0 / (sqrt(sum) + eps));
+    uint16_t h[4], l[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        h[k] = to_f16(x[k]);
+        l[k] = to_f16((x[k] - from_f16(h[k])) * kLoScale);
     }
-    __syncthreads();
-    const float inv = s_inv;
-    const int64_t per = cpad / 4, n = rpad * per;
-    for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < n;
-         q += (int64_t)gridDim.x * 256) {
-        const int64_t r = q / per, c = (q - r * per) * 4;
+    return Split4{make_uint2(pack(h[0], h[1]), pack(h[2], h[3])),
+                  make_uint2(pack(l[0], l[1]), pack(l[2], l[3]))};
+}
+// X_0 = x / (|x| + eps), padded with zeros to [rpad, cpad], scaled.
+template <bool kVec>
+__global__ __launch_bounds__(256) void normalise_kernel(Source s, int32_t rows, int32_t cols,
+                                                        int32_t rpad, int32_t cpad,
+                                                        const double* part, int32_t parts,
+                                                        double eps, float scale, uint16_t* hi,
+                                                        uint16_t* lo)
+{
+    __shared__ double s_sum[4];
+    const int64_t b = blockIdx.y;
+    double sum = 0.0;
+    for (int32_t k = threadIdx.x; k < parts; k += 256) sum += part[b * parts + k];
+    const float inv = (float)(1.0 / (sqrt(block_sum(sum, s_sum)) + eps));
+    const uint32_t per = (uint32_t)cpad / 4, n = (uint32_t)rpad * per;
+    hi += b * rpad * cpad;
+    lo += b * rpad * cpad;
+    for (uint32_t q = blockIdx.x * 256 + threadIdx.x; q < n; q += gridDim.x * 256) {
+        const int32_t r = (int32_t)(q / per), c = (int32_t)(q - r * per) * 4;
         f32x4 x = f32x4{0.f, 0.f, 0.f, 0.f};
-        if (r < rows) {
-            if (s.momentum) {
-                const int64_t at = (b * rows + r) * cols + c;
-#pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    if (c + k < cols)
-                        x[k] = muon_value(s, s.momentum[at + k], s.nesterov ? s.g[at + k] : 0.f);
-            } else {
-                const int64_t at = b * s.stride + r * s.ld + c;
-#pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    if (c + k < cols)
-                        x[k] = s.bf16 ? from_bf16(((const uint16_t*)s.x)[at + k])
-                                      : ((const float*)s.x)[at + k];
-            }
-        }
-        uint16_t h[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            x[k] *= inv;
-            h[k] = to_f16(x[k] * scale);
-        }
-        const int64_t o = b * rpad * cpad + r * cpad + c;
-        *(f32x4*)(x32 + o) = x;
-        *(uint2*)(x16 + o) =
-            make_uint2(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16);
+        if (r < rows && c < cols) x = values<kVec>(s, b, r, c, rows, cols) * inv;
+        const Split4 w = split(x * scale);
+        *(uint2*)(hi + (int64_t)q * 4) = w.hi;
+        *(uint2*)(lo + (int64_t)q * 4) = w.lo;
     }
 }
 
 // ---- epilogues -----------------------------------------------------------------
 
-// Square symmetric FP16 result [k, k]: scale * sum, or (B) lin * S + scale *
-// sum with S the factor.  Tiles above the diagonal are written twice, once
-// transposed.
+// S: scale * sum, square, symmetric, in FP16; and B = lin * S + scale * sum (the
+// sum being S S), likewise but for its diagonal, which goes to diag in
+// binary32 (unscaled) and is zero in B.  Tiles above the diagonal are written
+// twice, once transposed.
+template <bool kPoly>
 struct SquareEpi {
     struct Args {
         uint16_t* out;
-        const uint16_t* s;     // null: S itself
+        const uint16_t* s;
+        float* diag;           // [batch, ld]
         int64_t ld, stride;
-        float scale, lin;
+        float scale, lin, unscale;
+    };
+    struct Rows {
+        static constexpr bool kMirror = true, kAhead = true;
+        struct Regs {
+            uint4 s;
+        };
+        const Args& e;
+        uint16_t* out;
+        const uint16_t* s;
+        float* diag;
+        int64_t ni, nj;
+        __device__ __forceinline__ void columns(int64_t) const {}
+        __device__ __forceinline__ bool in(int64_t jj, int64_t ii) const
+        {
+            return jj < nj && ii < ni;
+        }
+        __device__ __forceinline__ void load(Regs& r, int64_t jj, int64_t ii) const
+        {
+            if constexpr (kPoly)
+                r.s = in(jj, ii) ? *(const uint4*)(s + jj * e.ld + ii) : make_uint4(0, 0, 0, 0);
+        }
+        __device__ __forceinline__ void put(const Regs& r, int64_t jj, int64_t ii,
+                                            float (&x)[8]) const
+        {
+            if (!in(jj, ii)) return;
+            if constexpr (kPoly) {
+                float y[8];
+                halves8(r.s, y);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    x[k] = x[k] * e.scale + y[k] * e.lin;
+                    if (ii + k == jj) {
+                        diag[jj] = x[k] * e.unscale;
+                        x[k] = 0.f;
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) x[k] *= e.scale;
+            }
+            *(uint4*)(out + jj * e.ld + ii) = f16x8(x);
+        }
+        __device__ __forceinline__ void mirror(int64_t ii, int64_t jj, const float (&y)[16]) const
+        {
+            if (!in(jj, ii)) return;
+            *(uint4*)(out + ii * e.ld + jj) = f16x8(y);
+            *(uint4*)(out + ii * e.ld + jj + 8) = f16x8(y + 8);
+        }
     };
     template <class S>
     static __device__ __forceinline__ void run(const Args& e, const pr::ProductArgs& p,
                                                const pr::TileAt& at, const pr::LanePos<S>& pos,
                                                f32x4 (&acc)[S::FI][S::FJ])
     {
-        uint16_t* out = e.out + at.batch * e.stride;
-        const uint16_t* s = e.s ? e.s + at.batch * e.stride : nullptr;
-        const bool mirror = p.symmetric && at.ti != at.tj;
+        const int64_t b = at.batch;
+        Rows f{e, e.out + b * e.stride, kPoly ? e.s + b * e.stride : nullptr,
+               kPoly ? e.diag + b * e.ld : nullptr, p.ni, p.nj};
+        pr::for_rows<S>(pos, acc, f, at.ti != at.tj);
+    }
+};
+
+// What the epilogues of X' = (a + diag) X + B X share: X in two parts, and the
+// diagonal along the rows (kWide) or the columns.
+struct LinearTerm {
+    const uint16_t *hi, *lo;
+    const float* diag;         // [batch, dld]
+    int64_t ld, stride, dld;
+    float a, unscale, scale;   // unscale: of X; scale: of the sum
+};
+template <bool kWide>
+struct LinearRows {
+    struct Regs {
+        uint4 hi, lo;
+        float d;
+    };
+    const LinearTerm& t;
+    int64_t batch;
+    float d[8];                // tall: of the lane's columns
+    __device__ __forceinline__ LinearRows(const LinearTerm& term, int64_t b) : t(term), batch(b) {}
+    __device__ __forceinline__ void columns(int64_t ii)
+    {
+        if constexpr (!kWide) {
 #pragma unroll
-        for (int j = 0; j < S::FJ; ++j) {
-            const int64_t jj = pos.j + 16 * j;
-            if (jj >= p.nj) continue;
+            for (int k = 0; k < 8; ++k) d[k] = ii < t.dld ? t.diag[batch * t.dld + ii + k] : 0.f;
+        }
+    }
+    __device__ __forceinline__ void load(Regs& r, int64_t jj, int64_t ii) const
+    {
+        const int64_t at = batch * t.stride + jj * t.ld + ii;
+        r.hi = *(const uint4*)(t.hi + at);
+        r.lo = *(const uint4*)(t.lo + at);
+        if constexpr (kWide) r.d = t.diag[batch * t.dld + jj];
+    }
+    __device__ __forceinline__ void update(const Regs& r, float (&x)[8]) const
+    {
+        float h[8], l[8];
+        halves8(r.hi, h);
+        halves8(r.lo, l);
 #pragma unroll
-            for (int i = 0; i < S::FI; ++i) {
-                const int64_t ii = pos.i + 16 * i;
-                if (ii >= p.ni) continue;
-                f32x4 x = acc[i][j] * e.scale;
-                if (s) {
-                    const uint2 w = *(const uint2*)(s + jj * e.ld + ii);
-                    x[0] += e.lin * from_f16((uint16_t)w.x);
-                    x[1] += e.lin * from_f16((uint16_t)(w.x >> 16));
-                    x[2] += e.lin * from_f16((uint16_t)w.y);
-                    x[3] += e.lin * from_f16((uint16_t)(w.y >> 16));
-                }
-                uint16_t h[4];
-#pragma unroll
-                for (int r = 0; r < 4; ++r) h[r] = to_f16(x[r]);
-                *(uint2*)(out + jj * e.ld + ii) =
-                    make_uint2(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16);
-                if (mirror)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) out[(ii + r) * e.ld + jj] = h[r];
-            }
+        for (int k = 0; k < 8; ++k) {
+            const float f = t.a + (kWide ? r.d : d[k]);
+            x[k] = (h[k] + l[k] * (1.f / kLoScale)) * t.unscale * f + x[k] * t.scale;
         }
     }
 };
 
-// X' = a X + sum, in binary32 (in place) and in FP16 for the next iteration.
+template <bool kWide>
 struct NextEpi {
     struct Args {
-        float* x32;
-        uint16_t* x16;
-        int64_t ld, stride;
-        float a, scale, next;
+        LinearTerm x;
+        uint16_t *hi, *lo;     // lo in place of x.lo
+        float next;
+    };
+    struct Rows {
+        static constexpr bool kMirror = false, kAhead = true;
+        typedef typename LinearRows<kWide>::Regs Regs;
+        const Args& e;
+        LinearRows<kWide> lin;
+        int64_t batch, ni, nj;
+        __device__ __forceinline__ void columns(int64_t ii) { lin.columns(ii); }
+        __device__ __forceinline__ void load(Regs& r, int64_t jj, int64_t ii) const
+        {
+            if (jj < nj && ii < ni) lin.load(r, jj, ii);
+        }
+        __device__ __forceinline__ void put(const Regs& r, int64_t jj, int64_t ii,
+                                            float (&x)[8]) const
+        {
+            if (jj >= nj || ii >= ni) return;
+            lin.update(r, x);
+            float l[8];
+            uint32_t h[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                x[k] *= e.next;
+                h[k] = to_f16(x[k]);
+                l[k] = (x[k] - from_f16((uint16_t)h[k])) * kLoScale;
+            }
+            const int64_t o = batch * e.x.stride + jj * e.x.ld + ii;
+            *(uint4*)(e.hi + o) = make_uint4(h[0] | h[1] << 16, h[2] | h[3] << 16,
+                                             h[4] | h[5] << 16, h[6] | h[7] << 16);
+            *(uint4*)(e.lo + o) = f16x8(l);
+        }
     };
     template <class S>
     static __device__ __forceinline__ void run(const Args& e, const pr::ProductArgs& p,
                                                const pr::TileAt& at, const pr::LanePos<S>& pos,
                                                f32x4 (&acc)[S::FI][S::FJ])
     {
-        float* x32 = e.x32 + at.batch * e.stride;
-        uint16_t* x16 = e.x16 + at.batch * e.stride;
-#pragma unroll
-        for (int j = 0; j < S::FJ; ++j) {
-            const int64_t jj = pos.j + 16 * j;
-            if (jj >= p.nj) continue;
-#pragma unroll
-            for (int i = 0; i < S::FI; ++i) {
-                const int64_t ii = pos.i + 16 * i;
-                if (ii >= p.ni) continue;
-                f32x4* q = (f32x4*)(x32 + jj * e.ld + ii);
-                const f32x4 x = *q * e.a + acc[i][j] * e.scale;
-                *q = x;
-                *(uint2*)(x16 + jj * e.ld + ii) =
-                    make_uint2(pack(to_f16(x[0] * e.next), to_f16(x[1] * e.next)),
-                               pack(to_f16(x[2] * e.next), to_f16(x[3] * e.next)));
-            }
-        }
+        Rows f{e, LinearRows<kWide>(e.x, at.batch), at.batch, p.ni, p.nj};
+        pr::for_rows<S>(pos, acc, f);
     }
 };
 
 // The last iteration: the result in BF16, and (kMuon) the weights' step.
-template <bool kMuon>
+template <bool kWide, bool kMuon>
 struct LastEpi {
     struct Args {
-        const float* x32;
-        int64_t ld, stride;    // of x32
-        float a, scale;
+        LinearTerm x;
         uint16_t* out;
         int64_t out_ld, out_stride;
         int32_t rows, cols;
-        int32_t vec, pvec;     // rows of out at 8-byte, of p at 16-byte addresses
+        int32_t vec;           // rows of out and p at 16-byte addresses
         float* p;              // [batch, rows, cols]
         float decay, rate;
+    };
+    struct Rows {
+        static constexpr bool kMirror = false, kAhead = !kMuon;   // (the registers it takes)
+        struct Regs {
+            typename LinearRows<kWide>::Regs x;
+            f32x4 p[kMuon ? 2 : 1];
+        };
+        const Args& e;
+        LinearRows<kWide> lin;
+        uint16_t* out;
+        float* p;
+        __device__ __forceinline__ void columns(int64_t ii) { lin.columns(ii); }
+        __device__ __forceinline__ void load(Regs& r, int64_t jj, int64_t ii) const
+        {
+            if (jj >= e.rows || ii >= e.cols) return;
+            lin.load(r.x, jj, ii);
+            if constexpr (kMuon) {
+                if (e.vec && ii + 8 <= e.cols) {
+                    const float* q = p + jj * e.cols + ii;
+                    r.p[0] = *(const f32x4*)q;
+                    r.p[1] = *(const f32x4*)(q + 4);
+                }
+            }
+        }
+        __device__ __forceinline__ void put(const Regs& r, int64_t jj, int64_t ii,
+                                            float (&x)[8]) const
+        {
+            if (jj >= e.rows || ii >= e.cols) return;
+            lin.update(r.x, x);
+            const uint4 w = bf16x8(x);
+            const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+            uint16_t* q = out + jj * e.out_ld + ii;
+            float* v = kMuon ? p + jj * e.cols + ii : nullptr;
+            if (e.vec && ii + 8 <= e.cols) {
+                *(uint4*)q = w;
+                if constexpr (kMuon) {
+#pragma unroll
+                    for (int k = 0; k < 8; k += 4) {
+                        f32x4 y;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            y[i] = e.decay * r.p[k >> 2][i] -
+                                   e.rate * from_bf16((uint16_t)(u[(k + i) >> 1] >> 16 * (i & 1)));
+                        *(f32x4*)(v + k) = y;
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (ii + k < e.cols) {
+                        const uint16_t o = (uint16_t)(u[k >> 1] >> 16 * (k & 1));
+                        q[k] = o;
+                        if constexpr (kMuon) v[k] = e.decay * v[k] - e.rate * from_bf16(o);
+                    }
+            }
+        }
     };
     template <class S>
     static __device__ __forceinline__ void run(const Args& e, const pr::ProductArgs& p,
                                                const pr::TileAt& at, const pr::LanePos<S>& pos,
                                                f32x4 (&acc)[S::FI][S::FJ])
     {
-        const float* x32 = e.x32 + at.batch * e.stride;
-        uint16_t* out = e.out + at.batch * e.out_stride;
-        float* w = kMuon ? e.p + at.batch * (int64_t)e.rows * e.cols : nullptr;
-#pragma unroll
-        for (int j = 0; j < S::FJ; ++j) {
-            const int64_t jj = pos.j + 16 * j;
-            if (jj >= e.rows) continue;
-#pragma unroll
-            for (int i = 0; i < S::FI; ++i) {
-                const int64_t ii = pos.i + 16 * i;
-                if (ii >= e.cols) continue;
-                const f32x4 x = *(const f32x4*)(x32 + jj * e.ld + ii) * e.a + acc[i][j] * e.scale;
-                const uint32_t lo = pack(to_bf16(x[0]), to_bf16(x[1]));
-                const uint32_t hi = pack(to_bf16(x[2]), to_bf16(x[3]));
-                const f32x4 o = f32x4{from_bf16((uint16_t)lo), from_bf16((uint16_t)(lo >> 16)),
-                                      from_bf16((uint16_t)hi), from_bf16((uint16_t)(hi >> 16))};
-                const bool whole = ii + 4 <= e.cols;
-                uint16_t* q = out + jj * e.out_ld + ii;
-                if (e.vec && whole) {
-                    *(uint2*)q = make_uint2(lo, hi);
-                } else {
-                    q[0] = (uint16_t)lo;
-                    if (ii + 1 < e.cols) q[1] = (uint16_t)(lo >> 16);
-                    if (ii + 2 < e.cols) q[2] = (uint16_t)hi;
-                    if (ii + 3 < e.cols) q[3] = (uint16_t)(hi >> 16);
-                }
-                if constexpr (kMuon) {
-                    float* v = w + jj * e.cols + ii;
-                    if (e.pvec && whole) {
-                        *(f32x4*)v = *(const f32x4*)v * e.decay - o * e.rate;
-                    } else {
-#pragma unroll
-                        for (int r = 0; r < 4; ++r)
-                            if (ii + r < e.cols) v[r] = e.decay * v[r] - e.rate * o[r];
-                    }
-                }
-            }
-        }
+        Rows f{e, LinearRows<kWide>(e.x, at.batch), e.out + at.batch * e.out_stride,
+               kMuon ? e.p + at.batch * (int64_t)e.rows * e.cols : nullptr};
+        pr::for_rows<S>(pos, acc, f);
     }
 };
 
@@ -380,20 +542,31 @@ bool orth_sizes(int64_t batch, int64_t rows, int64_t cols, OrthSizes* z)
 
 struct OrthBuffers {
     double* part;
-    float* x32;
-    uint16_t *x16[2], *s, *b;
+    uint16_t *hi[2], *lo, *s, *b;
+    float* diag;
 };
+
+// Blocks per matrix that sum its squares: 4096 values each, until the chip is
+// full.
+int64_t norm_parts(const OrthSizes& z)
+{
+    int64_t parts = div_up(z.rows * z.cols, 4096);
+    const int64_t most = div_up(4096, z.batch);
+    if (parts > most) parts = most;
+    return parts > kMaxParts ? kMaxParts : parts;
+}
 
 int64_t carve(const OrthSizes& z, void* ws, OrthBuffers* b)
 {
     Carver c(ws);
     const int64_t n = z.batch * z.rpad * z.cpad, k = z.batch * z.kpad * z.kpad;
-    b->part = c.take<double>(z.batch * kNormBlocks);
-    b->x32 = c.take<float>(n);
-    b->x16[0] = c.take<uint16_t>(n);
-    b->x16[1] = c.take<uint16_t>(n);
+    b->part = c.take<double>(z.batch * norm_parts(z));
+    b->hi[0] = c.take<uint16_t>(n);
+    b->hi[1] = c.take<uint16_t>(n);
+    b->lo = c.take<uint16_t>(n);
     b->s = c.take<uint16_t>(k);
     b->b = c.take<uint16_t>(k);
+    b->diag = c.take<float>(z.batch * z.kpad);
     return c.used;
 }
 
@@ -422,96 +595,116 @@ struct Muon {
     float decay, rate;
 };
 
-hipError_t orthogonalise(const Source& src, const OrthSizes& z, const dte_newton_schulz& ns,
-                         const Bounds& bd, uint16_t* out, int64_t out_ld, int64_t out_stride,
-                         const Muon* muon, const OrthBuffers& b, hipStream_t st)
-{
-    const int64_t n = z.rpad * z.cpad;
-    int64_t parts = div_up(z.rows * z.cols, 4096);
-    if (!src.momentum && parts > z.rows) parts = z.rows;
-    if (parts > kNormBlocks) parts = kNormBlocks;
-    norm_kernel<<<dim3((unsigned)parts, (unsigned)z.batch), dim3(256), 0, st>>>(
-        src, (int32_t)z.rows, (int32_t)z.cols, b.part);
-    hipError_t err = hipGetLastError();
-    if (err != hipSuccess) return err;
-    int64_t blocks = div_up(n / 4, 256);
-    const int64_t most = div_up(4096, z.batch);
-    if (blocks > most) blocks = most;
-    double xs = fp16_scale(bd.sigma[0]);
-    normalise_kernel<<<dim3((unsigned)blocks, (unsigned)z.batch), dim3(256), 0, st>>>(
-        src, (int32_t)z.rows, (int32_t)z.cols, z.rpad, z.cpad, b.part, (int32_t)parts, ns.eps,
-        (float)xs, b.x32, b.x16[0]);
-    err = hipGetLastError();
-    if (err != hipSuccess) return err;
+struct Result {
+    uint16_t* out;
+    int64_t ld, stride;
+    const Muon* muon;
+};
 
+template <bool kWide>
+hipError_t last_product(const pr::ProductArgs& u, const LinearTerm& x, const OrthSizes& z,
+                        const Result& o, hipStream_t st)
+{
+    constexpr pr::Layout kA = kWide ? pr::kR : pr::kK;
+    int32_t vec = rows_aligned(o.out, o.ld, 2, 16) && o.stride % 8 == 0;
+    if (o.muon) {
+        vec = vec && rows_aligned(o.muon->p, z.cols, 4, 16) && z.rows * z.cols % 4 == 0;
+        const typename LastEpi<kWide, true>::Args e{x, o.out, o.ld, o.stride, (int32_t)z.rows,
+                                                    (int32_t)z.cols, vec, o.muon->p,
+                                                    o.muon->decay, o.muon->rate};
+        return product<kA, pr::kK, LastEpi<kWide, true>>(u, e, st);
+    }
+    const typename LastEpi<kWide, false>::Args e{
+        x, o.out, o.ld, o.stride, (int32_t)z.rows, (int32_t)z.cols, vec, nullptr, 0.f, 0.f};
+    return product<kA, pr::kK, LastEpi<kWide, false>>(u, e, st);
+}
+
+template <bool kWide>
+hipError_t iterate(const OrthSizes& z, const dte_newton_schulz& ns, const Bounds& bd,
+                   const OrthBuffers& b, const Result& o, hipStream_t st)
+{
+    constexpr pr::Layout kXrow = kWide ? pr::kK : pr::kR;   // X as a factor of S
+    const int64_t n = z.rpad * z.cpad, kk = z.kpad * z.kpad;
+    double xs = fp16_scale(bd.sigma[0]);
     for (int k = 0; k < ns.steps; ++k) {
-        const uint16_t* x = b.x16[k & 1];
         const double ss = fp16_scale(bd.sigma[k] * bd.sigma[k]), bs = fp16_scale(bd.b[k]);
-        const double a = ns.coefficients[k][0], bc = ns.coefficients[k][1],
-                     cc = ns.coefficients[k][2];
-        const int64_t kk = z.kpad * z.kpad;
-        // S
+        const double bc = ns.coefficients[k][1], cc = ns.coefficients[k][2];
+        // X's rows along the smaller side, and along the other
+        const pr::Operand x{b.hi[k & 1], z.cpad, n, (int32_t)(kWide ? z.rpad : z.cpad), 0, 0};
+        const pr::Operand xt{b.hi[k & 1], z.cpad, n, (int32_t)(kWide ? z.cpad : z.rpad), 0, 0};
+        const pr::Operand s{b.s, z.kpad, kk, (int32_t)z.kpad, 0, 0};
+        const pr::Operand bm{b.b, z.kpad, kk, (int32_t)z.kpad, 0, 0};
         pr::ProductArgs p{};
-        p.a = p.b = z.wide ? pr::Operand{x, z.cpad, n, (int32_t)z.rpad, (int32_t)z.cpad, 0}
-                           : pr::Operand{x, z.cpad, n, (int32_t)z.cpad, (int32_t)z.rpad, 0};
+        p.a = p.b = x;
         p.ni = p.nj = (int32_t)z.kpad;
-        p.steps = (int32_t)((z.wide ? z.cpad : z.rpad) / 64);
+        p.steps = (int32_t)((kWide ? z.cpad : z.rpad) / 64);
         p.split = 1;
         p.batch = (int32_t)z.batch;
         p.symmetric = 1;
-        const SquareEpi::Args es{b.s, nullptr, z.kpad, kk, (float)(ss / (xs * xs)), 0.f};
-        err = z.wide ? product<pr::kK, pr::kK, SquareEpi>(p, es, st)
-                     : product<pr::kR, pr::kR, SquareEpi>(p, es, st);
+        const SquareEpi<false>::Args eg{b.s, nullptr, nullptr, z.kpad, kk,
+                                        (float)(ss / (xs * xs)), 0.f, 0.f};
+        hipError_t err = product<kXrow, kXrow, SquareEpi<false>>(p, eg, st);
         if (err != hipSuccess) return err;
-        // B = b S + c S S
-        p.a = p.b = pr::Operand{b.s, z.kpad, kk, (int32_t)z.kpad, (int32_t)z.kpad, 0};
+        p.a = p.b = s;
         p.steps = (int32_t)(z.kpad / 64);
-        const SquareEpi::Args eb{b.b, b.s, z.kpad, kk, (float)(cc * bs / (ss * ss)),
-                                 (float)(bc * bs / ss)};
-        err = product<pr::kK, pr::kK, SquareEpi>(p, eb, st);
+        const SquareEpi<true>::Args ep{b.b, b.s, b.diag, z.kpad, kk, (float)(cc * bs / (ss * ss)),
+                                       (float)(bc * bs / ss), (float)(1.0 / bs)};
+        err = product<pr::kK, pr::kK, SquareEpi<true>>(p, ep, st);
         if (err != hipSuccess) return err;
-        // X
-        const bool last = k + 1 == ns.steps;
-        const double next = last ? 1.0 : fp16_scale(bd.sigma[k + 1]);
-        const pr::Operand bm{b.b, z.kpad, kk, (int32_t)z.kpad, (int32_t)z.kpad, 0};
+
+        // wide: out[j, i] = sum_k X[k, i] B[j, k]; tall: sum_k B[i, k] X[j, k]
+        constexpr pr::Layout kA = kWide ? pr::kR : pr::kK;
         pr::ProductArgs u{};
+        u.a = kWide ? xt : bm;
+        u.b = kWide ? bm : xt;
         u.ni = (int32_t)z.cpad;
         u.nj = (int32_t)z.rpad;
         u.steps = (int32_t)(z.kpad / 64);
         u.split = 1;
         u.batch = (int32_t)z.batch;
-        if (z.wide) {      // out[j, i] = sum_k X[k, i] B[j, k]
-            u.a = pr::Operand{x, z.cpad, n, (int32_t)z.cpad, (int32_t)z.rpad, 0};
-            u.b = bm;
-        } else {           // out[j, i] = sum_k B[i, k] X[j, k]
-            u.a = bm;
-            u.b = pr::Operand{x, z.cpad, n, (int32_t)z.rpad, (int32_t)z.cpad, 0};
-        }
-        const float scale = (float)(1.0 / (bs * xs));
-        if (!last) {
-            const NextEpi::Args e{b.x32, b.x16[(k + 1) & 1], z.cpad, n, (float)a, scale,
-                                  (float)next};
-            err = z.wide ? product<pr::kR, pr::kK, NextEpi>(u, e, st)
-                         : product<pr::kK, pr::kK, NextEpi>(u, e, st);
-        } else if (muon) {
-            const LastEpi<true>::Args e{
-                b.x32, z.cpad, n, (float)a, scale, out, out_ld, out_stride, (int32_t)z.rows,
-                (int32_t)z.cols, rows_aligned(out, out_ld, 2, 8) && out_stride % 4 == 0,
-                rows_aligned(muon->p, z.cols, 4, 16), muon->p, muon->decay, muon->rate};
-            err = z.wide ? product<pr::kR, pr::kK, LastEpi<true>>(u, e, st)
-                         : product<pr::kK, pr::kK, LastEpi<true>>(u, e, st);
-        } else {
-            const LastEpi<false>::Args e{
-                b.x32, z.cpad, n, (float)a, scale, out, out_ld, out_stride, (int32_t)z.rows,
-                (int32_t)z.cols, rows_aligned(out, out_ld, 2, 8) && out_stride % 4 == 0, 0,
-                nullptr, 0.f, 0.f};
-            err = z.wide ? product<pr::kR, pr::kK, LastEpi<false>>(u, e, st)
-                         : product<pr::kK, pr::kK, LastEpi<false>>(u, e, st);
-        }
+        const LinearTerm lin{b.hi[k & 1], b.lo, b.diag, z.cpad, n, z.kpad,
+                             (float)ns.coefficients[k][0], (float)(1.0 / xs),
+                             (float)(1.0 / (bs * xs))};
+        if (k + 1 == ns.steps) return last_product<kWide>(u, lin, z, o, st);
+        xs = fp16_scale(bd.sigma[k + 1]);
+        const typename NextEpi<kWide>::Args en{lin, b.hi[(k + 1) & 1], b.lo, (float)xs};
+        err = product<kA, pr::kK, NextEpi<kWide>>(u, en, st);
         if (err != hipSuccess) return err;
-        xs = next;
     }
     return hipSuccess;
+}
+
+hipError_t orthogonalise(const Source& src, const OrthSizes& z, const dte_newton_schulz& ns,
+                         const Bounds& bd, const Result& o, const OrthBuffers& b, hipStream_t st)
+{
+    const int32_t parts = (int32_t)norm_parts(z);
+    const dim3 block(256), ngrid((unsigned)parts, (unsigned)z.batch);
+    int64_t blocks = div_up(z.rpad * z.cpad / 4, 256);
+    const int64_t most = div_up(8192, z.batch);
+    if (blocks > most) blocks = most;
+    const dim3 xgrid((unsigned)blocks, (unsigned)z.batch);
+    const int32_t rows = (int32_t)z.rows, cols = (int32_t)z.cols;
+    bool vec = cols % 4 == 0;
+    if (src.momentum)
+        vec = vec && rows_aligned(src.momentum, cols, 4, 16) && rows_aligned(src.g, cols, 4, 16);
+    else
+        vec = vec && rows_aligned(src.x, src.ld, src.bf16 ? 2 : 4, src.bf16 ? 8 : 16) &&
+              src.stride % 4 == 0;
+    const float xs = (float)fp16_scale(bd.sigma[0]);
+    if (vec) {
+        norm_kernel<true><<<ngrid, block, 0, st>>>(src, rows, cols, b.part);
+        normalise_kernel<true><<<xgrid, block, 0, st>>>(src, rows, cols, (int32_t)z.rpad,
+                                                        (int32_t)z.cpad, b.part, parts, ns.eps, xs,
+                                                        b.hi[0], b.lo);
+    } else {
+        norm_kernel<false><<<ngrid, block, 0, st>>>(src, rows, cols, b.part);
+        normalise_kernel<false><<<xgrid, block, 0, st>>>(src, rows, cols, (int32_t)z.rpad,
+                                                         (int32_t)z.cpad, b.part, parts, ns.eps,
+                                                         xs, b.hi[0], b.lo);
+    }
+    const hipError_t err = hipGetLastError();
+    if (err != hipSuccess) return err;
+    return z.wide ? iterate<true>(z, ns, bd, b, o, st) : iterate<false>(z, ns, bd, b, o, st);
 }
 
 }  // namespace
@@ -548,7 +741,7 @@ dte_status dte_orthogonalise(const void* x, int32_t x_type, int64_t batch, int64
     if (!workspace_ok(workspace, workspace_bytes, dte::carve(z, workspace, &b)))
         return DTE_ERR_ARG;
     const dte::Source src{x, x_ld, x_stride, x_type == DTE_TYPE_BF16, nullptr, nullptr, 0.f, 0};
-    return dte::orthogonalise(src, z, *ns, bd, out, out_ld, out_stride, nullptr, b,
+    return dte::orthogonalise(src, z, *ns, bd, dte::Result{out, out_ld, out_stride, nullptr}, b,
                               (hipStream_t)stream) == hipSuccess
                ? DTE_OK
                : DTE_ERR_HIP;
@@ -577,7 +770,7 @@ dte_status dte_muon_forward(float* p, float* momentum, const float* g, int64_t b
     const dte::Source src{nullptr, cols, rows * cols, 0, momentum, g, (float)hp->momentum,
                           hp->nesterov != 0};
     const dte::Muon muon{p, (float)decay, (float)rate};
-    return dte::orthogonalise(src, z, hp->ns, bd, update, cols, rows * cols, &muon, b,
+    return dte::orthogonalise(src, z, hp->ns, bd, dte::Result{update, cols, rows * cols, &muon}, b,
                               (hipStream_t)stream) == hipSuccess
                ? DTE_OK
                : DTE_ERR_HIP;

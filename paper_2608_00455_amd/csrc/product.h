@@ -298,7 +298,7 @@ template <class S, bool kF16, Layout kA, Layout kB>
 __device__ __forceinline__ void tile_product(const ProductArgs& p, const TileAt& at, int wave,
                                              f32x4 (&acc)[S::FI][S::FJ])
 {
-    constexpr uint32_t kStage = S::kStageBytes, kBAt = S::TI * kStepK * 2;
+    [[maybe_unused]] constexpr uint32_t kStage = S::kStageBytes, kBAt = S::TI * kStepK * 2;
     const int32_t per = (p.steps + p.split - 1) / p.split;
     const int32_t s0 = at.split * per, s1 = min(p.steps, s0 + per);
 #pragma unroll
@@ -403,6 +403,79 @@ struct LanePos {
         j = (int64_t)at.tj * S::TJ + w / S::kWI * S::FJ * 16 + (lane & 15);
     }
 };
+
+// The sums of a wave, eight consecutive i of one j at a time: f.load(regs, j, i)
+// fetches what f.put(regs, j, i, x) needs beside them, a group of 16 j before it
+// is used; f.columns(i) is told once which i the lane will see.
+// A lane's sums are four i of one j, and 16 lanes hold 16 different j: written
+// as they are, a store instruction touches 16 rows with 32 or 64 bytes of each,
+// and loads and stores of one lane follow one another.  So each group of 16 j
+// goes through LDS (each wave its own part, no barrier) and comes back row by
+// row: 16-byte accesses, 128 or 256 contiguous bytes per row.  (X' = a X + B X
+// of 128 matrices of 768 x 2048: 775 -> 400 us.)  With F::kMirror, put leaves
+// in x the values to be written transposed: f.mirror(i, j, y) takes 16
+// consecutive j of one i.
+template <class S, class F>
+__device__ __forceinline__ void for_rows(const LanePos<S>& pos, f32x4 (&acc)[S::FI][S::FJ], F& f,
+                                         bool mirror = false)
+{
+    constexpr int kWide = S::FI * 16, kPitch = kWide + 4;
+    constexpr int kLanes = kWide / 8, kRows = 64 / kLanes, kPasses = 16 / kRows;
+    static_assert(S::kWI * S::kWJ * 16 * kPitch * 4 <= S::kLds, "the parts fit the tiles' LDS");
+    const int lane = pos.lane;
+    float* part = (float*)s_dynamic + pos.wave * 16 * kPitch;
+    const int64_t i0 = pos.i - 4 * (lane >> 4), j0 = pos.j - (lane & 15);
+    const int row = lane / kLanes, col = (lane % kLanes) * 8;
+    // F::kAhead: the next group's values are fetched before this one is done
+    typename F::Regs regs[F::kAhead ? 2 : 1][kPasses];
+    f.columns(i0 + col);
+#pragma unroll
+    for (int k = 0; k < kPasses; ++k) f.load(regs[0][k], j0 + row + k * kRows, i0 + col);
+#pragma unroll
+    for (int j = 0; j < S::FJ; ++j) {
+        const int now = F::kAhead ? j & 1 : 0;
+#pragma unroll
+        for (int i = 0; i < S::FI; ++i)
+            *(f32x4*)(part + (lane & 15) * kPitch + i * 16 + 4 * (lane >> 4)) = acc[i][j];
+        if (F::kAhead && j + 1 < S::FJ) {
+#pragma unroll
+            for (int k = 0; k < kPasses; ++k)
+                f.load(regs[1 - now][k], j0 + 16 * (j + 1) + row + k * kRows, i0 + col);
+        }
+        asm volatile("" ::: "memory");   // LDS operations of a wave are in order
+#pragma unroll
+        for (int k = 0; k < kPasses; ++k) {
+            float* at = part + (row + k * kRows) * kPitch + col;
+            const f32x4 lo = *(const f32x4*)at, hi = *(const f32x4*)(at + 4);
+            float x[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+            f.put(regs[now][k], j0 + 16 * j + row + k * kRows, i0 + col, x);
+            if constexpr (F::kMirror) {
+                if (mirror) {
+                    *(f32x4*)at = f32x4{x[0], x[1], x[2], x[3]};
+                    *(f32x4*)(at + 4) = f32x4{x[4], x[5], x[6], x[7]};
+                }
+            }
+        }
+        asm volatile("" ::: "memory");
+        if constexpr (F::kMirror) {
+            if (mirror) {
+#pragma unroll
+                for (int k = 0; k < kWide / 64; ++k) {
+                    float y[16];
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) y[r] = part[r * kPitch + k * 64 + lane];
+                    f.mirror(i0 + k * 64 + lane, j0 + 16 * j, y);
+                }
+                asm volatile("" ::: "memory");
+            }
+        }
+        if (!F::kAhead && j + 1 < S::FJ) {
+#pragma unroll
+            for (int k = 0; k < kPasses; ++k)
+                f.load(regs[0][k], j0 + 16 * (j + 1) + row + k * kRows, i0 + col);
+        }
+    }
+}
 
 // Epi::run(args, product, at, pos, acc) takes the sums.
 template <class S, bool kF16, Layout kA, Layout kB, class Epi>

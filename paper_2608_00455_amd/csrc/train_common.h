@@ -55,5 +55,16 @@ __device__ __forceinline__ float from_bf16(uint16_t x)
     return __builtin_bit_cast(float, (uint32_t)x << 16);
 }
 
+__device__ __forceinline__ uint32_t pack(uint16_t lo, uint16_t hi)
+{
+    return lo | (uint32_t)hi << 16;
+}
+// Eight values as BF16.
+__device__ __forceinline__ uint4 bf16x8(const float (&x)[8])
+{
+    return make_uint4(pack(to_bf16(x[0]), to_bf16(x[1])), pack(to_bf16(x[2]), to_bf16(x[3])),
+                      pack(to_bf16(x[4]), to_bf16(x[5])), pack(to_bf16(x[6]), to_bf16(x[7])));
+}
+
 }  // namespace tr
 }  // namespace dte
