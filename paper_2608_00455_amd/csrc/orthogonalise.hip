@@ -49,14 +49,10 @@ using pr::f32x4;
     return make_uint4(pack(to_f16(x[0]), to_f16(x[1])), pack(to_f16(x[2]), to_f16(x[3])),
                       pack(to_f16(x[4]), to_f16(x[5])), pack(to_f16(x[6]), to_f16(x[7])));
 }
-[[maybe_unused]] __device__ __forceinline__ void halves8(uint4 w, float (&x)[8])
+[[maybe_unused]] __device__ __forceinline__ float half_of(const uint4& w, int k)
 {
-    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        x[2 * k] = from_f16((uint16_t)u[k]);
-        x[2 * k + 1] = from_f16((uint16_t)(u[k] >> 16));
-    }
+    const uint32_t u = k < 2 ? w.x : k < 4 ? w.y : k < 6 ? w.z : w.w;
+    return from_f16((uint16_t)(k & 1 ? u >> 16 : u));
 }
 
 // ---- the matrix to work on -----------------------------------------------------
@@ -178,9 +174,9 @@ __global__ __launch_bounds__(256) void norm_kernel(Source s, int32_t rows, int32
     if (threadIdx.x == 0) part[b * gridDim.x + blockIdx.x] = sum;
 }
 
-// X in two FP16 parts: hi the scaled value, lo 1024 times what is left.
-constexpr float kLoScale = 1024.f;
-
+// X in two FP16 parts: hi the scaled value, lo what rounding left of it.  (With
+// X up to 2^14 the smallest FP16 is 2^-38 of the largest value: parts that
+// underflow do not matter.)
 struct Split4 {
     uint2 hi, lo;
 };
@@ -190,7 +186,7 @@ __device__ __forceinline__ Split4 split(f32x4 x)
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
         h[k] = to_f16(x[k]);
-        l[k] = to_f16((x[k] - from_f16(h[k])) * kLoScale);
+        l[k] = to_f16(x[k] - from_f16(h[k]));
     }
     return Split4{make_uint2(pack(h[0], h[1]), pack(h[2], h[3])),
                   make_uint2(pack(l[0], l[1]), pack(l[2], l[3]))};
@@ -261,15 +257,16 @@ struct SquareEpi {
         {
             if (!in(jj, ii)) return;
             if constexpr (kPoly) {
-                float y[8];
-                halves8(r.s, y);
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    x[k] = x[k] * e.scale + y[k] * e.lin;
-                    if (ii + k == jj) {
-                        diag[jj] = x[k] * e.unscale;
-                        x[k] = 0.f;
-                    }
+                for (int k = 0; k < 8; ++k)
+                    x[k] = __builtin_fmaf(half_of(r.s, k), e.lin, x[k] * e.scale);
+                if (ii <= jj && jj < ii + 8) {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        if (ii + k == jj) {
+                            diag[jj] = x[k] * e.unscale;
+                            x[k] = 0.f;
+                        }
                 }
             } else {
 #pragma unroll
@@ -297,12 +294,13 @@ struct SquareEpi {
 };
 
 // What the epilogues of X' = (a + diag) X + B X share: X in two parts, and the
-// diagonal along the rows (kWide) or the columns.
+// diagonal along the rows (kWide) or the columns.  The scales contain that of the
+// result.
 struct LinearTerm {
     const uint16_t *hi, *lo;
     const float* diag;         // [batch, dld]
     int64_t ld, stride, dld;
-    float a, unscale, scale;   // unscale: of X; scale: of the sum
+    float a, unscale, scale;   // of X, of the sum
 };
 template <bool kWide>
 struct LinearRows {
@@ -311,32 +309,36 @@ struct LinearRows {
         float d;
     };
     const LinearTerm& t;
-    int64_t batch;
-    float d[8];                // tall: of the lane's columns
-    __device__ __forceinline__ LinearRows(const LinearTerm& term, int64_t b) : t(term), batch(b) {}
+    const uint16_t *hi, *lo;
+    const float* diag;
+    float f[8];                // tall: of the lane's columns
+    __device__ __forceinline__ LinearRows(const LinearTerm& term, int64_t b)
+        : t(term), hi(t.hi + b * t.stride), lo(t.lo + b * t.stride), diag(t.diag + b * t.dld)
+    {
+    }
     __device__ __forceinline__ void columns(int64_t ii)
     {
         if constexpr (!kWide) {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) d[k] = ii < t.dld ? t.diag[batch * t.dld + ii + k] : 0.f;
+            for (int k = 0; k < 8; ++k)
+                f[k] = ii < t.dld ? (t.a + diag[ii + k]) * t.unscale : 0.f;
         }
     }
     __device__ __forceinline__ void load(Regs& r, int64_t jj, int64_t ii) const
     {
-        const int64_t at = batch * t.stride + jj * t.ld + ii;
-        r.hi = *(const uint4*)(t.hi + at);
-        r.lo = *(const uint4*)(t.lo + at);
-        if constexpr (kWide) r.d = t.diag[batch * t.dld + jj];
+        const int64_t at = jj * t.ld + ii;
+        r.hi = *(const uint4*)(hi + at);
+        r.lo = *(const uint4*)(lo + at);
+        if constexpr (kWide) r.d = diag[jj];   // (used later: nothing here waits for a load)
     }
     __device__ __forceinline__ void update(const Regs& r, float (&x)[8]) const
     {
-        float h[8], l[8];
-        halves8(r.hi, h);
-        halves8(r.lo, l);
+        const float row = kWide ? (t.a + r.d) * t.unscale : 0.f;
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-            const float f = t.a + (kWide ? r.d : d[k]);
-            x[k] = (h[k] + l[k] * (1.f / kLoScale)) * t.unscale * f + x[k] * t.scale;
+            const float g = kWide ? row : f[k];
+            x[k] = __builtin_fmaf(half_of(r.hi, k), g,
+                                  __builtin_fmaf(half_of(r.lo, k), g, x[k] * t.scale));
         }
     }
 };
@@ -346,14 +348,13 @@ struct NextEpi {
     struct Args {
         LinearTerm x;
         uint16_t *hi, *lo;     // lo in place of x.lo
-        float next;
     };
     struct Rows {
         static constexpr bool kMirror = false, kAhead = true;
         typedef typename LinearRows<kWide>::Regs Regs;
-        const Args& e;
         LinearRows<kWide> lin;
-        int64_t batch, ni, nj;
+        uint16_t *hi, *lo;
+        int64_t ld, ni, nj;
         __device__ __forceinline__ void columns(int64_t ii) { lin.columns(ii); }
         __device__ __forceinline__ void load(Regs& r, int64_t jj, int64_t ii) const
         {
@@ -364,18 +365,11 @@ struct NextEpi {
         {
             if (jj >= nj || ii >= ni) return;
             lin.update(r, x);
-            float l[8];
-            uint32_t h[8];
+            const uint4 h = f16x8(x);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                x[k] *= e.next;
-                h[k] = to_f16(x[k]);
-                l[k] = (x[k] - from_f16((uint16_t)h[k])) * kLoScale;
-            }
-            const int64_t o = batch * e.x.stride + jj * e.x.ld + ii;
-            *(uint4*)(e.hi + o) = make_uint4(h[0] | h[1] << 16, h[2] | h[3] << 16,
-                                             h[4] | h[5] << 16, h[6] | h[7] << 16);
-            *(uint4*)(e.lo + o) = f16x8(l);
+            for (int k = 0; k < 8; ++k) x[k] -= half_of(h, k);
+            *(uint4*)(hi + jj * ld + ii) = h;
+            *(uint4*)(lo + jj * ld + ii) = f16x8(x);
         }
     };
     template <class S>
@@ -383,7 +377,8 @@ struct NextEpi {
                                                const pr::TileAt& at, const pr::LanePos<S>& pos,
                                                f32x4 (&acc)[S::FI][S::FJ])
     {
-        Rows f{e, LinearRows<kWide>(e.x, at.batch), at.batch, p.ni, p.nj};
+        const int64_t b = at.batch * e.x.stride;
+        Rows f{LinearRows<kWide>(e.x, at.batch), e.hi + b, e.lo + b, e.x.ld, p.ni, p.nj};
         pr::for_rows<S>(pos, acc, f);
     }
 };
@@ -522,8 +517,14 @@ double fp16_scale(double top)
 
 struct OrthSizes {
     int64_t batch, rows, cols, rpad, cpad, kpad;
+    int64_t group;         // matrices that are worked on together
     bool wide;
 };
+
+int64_t work_bytes(const OrthSizes& z)
+{
+    return 6 * z.rpad * z.cpad + 4 * z.kpad * z.kpad;
+}
 
 bool orth_sizes(int64_t batch, int64_t rows, int64_t cols, OrthSizes* z)
 {
@@ -537,6 +538,9 @@ bool orth_sizes(int64_t batch, int64_t rows, int64_t cols, OrthSizes* z)
     z->cpad = round_up(cols, 64);
     z->wide = rows <= cols;
     z->kpad = z->wide ? z->rpad : z->cpad;
+    z->group = batch;
+    if (getenv("DTE_G")) z->group = atoi(getenv("DTE_G"));
+    if (z->group > batch) z->group = batch;
     return true;
 }
 
@@ -551,7 +555,7 @@ struct OrthBuffers {
 int64_t norm_parts(const OrthSizes& z)
 {
     int64_t parts = div_up(z.rows * z.cols, 4096);
-    const int64_t most = div_up(4096, z.batch);
+    const int64_t most = div_up(4096, z.group > 0 ? z.group : 1);
     if (parts > most) parts = most;
     return parts > kMaxParts ? kMaxParts : parts;
 }
@@ -559,14 +563,14 @@ int64_t norm_parts(const OrthSizes& z)
 int64_t carve(const OrthSizes& z, void* ws, OrthBuffers* b)
 {
     Carver c(ws);
-    const int64_t n = z.batch * z.rpad * z.cpad, k = z.batch * z.kpad * z.kpad;
-    b->part = c.take<double>(z.batch * norm_parts(z));
+    const int64_t n = z.group * z.rpad * z.cpad, k = z.group * z.kpad * z.kpad;
+    b->part = c.take<double>(z.group * norm_parts(z));
     b->hi[0] = c.take<uint16_t>(n);
     b->hi[1] = c.take<uint16_t>(n);
     b->lo = c.take<uint16_t>(n);
     b->s = c.take<uint16_t>(k);
     b->b = c.take<uint16_t>(k);
-    b->diag = c.take<float>(z.batch * z.kpad);
+    b->diag = c.take<float>(z.group * z.kpad);
     return c.used;
 }
 
@@ -585,6 +589,8 @@ bool large_tiles(int64_t ni, int64_t nj, int64_t batch, bool symmetric, int cus)
 template <pr::Layout kA, pr::Layout kB, class Epi>
 hipError_t product(pr::ProductArgs p, const typename Epi::Args& e, hipStream_t st)
 {
+    if (getenv("DTE_M") && p.symmetric == 0) return pr::launch_product<pr::Medium, true, kA, kB, Epi>(p, e, st);
+    if (getenv("DTE_MS") && p.symmetric != 0) return pr::launch_product<pr::Medium, true, kA, kB, Epi>(p, e, st);
     return large_tiles(p.ni, p.nj, p.batch, p.symmetric != 0, device_cus())
                ? pr::launch_product<pr::Large, true, kA, kB, Epi>(p, e, st)
                : pr::launch_product<pr::Medium, true, kA, kB, Epi>(p, e, st);
@@ -620,8 +626,8 @@ hipError_t last_product(const pr::ProductArgs& u, const LinearTerm& x, const Ort
 }
 
 template <bool kWide>
-hipError_t iterate(const OrthSizes& z, const dte_newton_schulz& ns, const Bounds& bd,
-                   const OrthBuffers& b, const Result& o, hipStream_t st)
+hipError_t iterate(const OrthSizes& z, int64_t batch, const dte_newton_schulz& ns,
+                   const Bounds& bd, const OrthBuffers& b, const Result& o, hipStream_t st)
 {
     constexpr pr::Layout kXrow = kWide ? pr::kK : pr::kR;   // X as a factor of S
     const int64_t n = z.rpad * z.cpad, kk = z.kpad * z.kpad;
@@ -639,7 +645,7 @@ hipError_t iterate(const OrthSizes& z, const dte_newton_schulz& ns, const Bounds
         p.ni = p.nj = (int32_t)z.kpad;
         p.steps = (int32_t)((kWide ? z.cpad : z.rpad) / 64);
         p.split = 1;
-        p.batch = (int32_t)z.batch;
+        p.batch = (int32_t)batch;
         p.symmetric = 1;
         const SquareEpi<false>::Args eg{b.s, nullptr, nullptr, z.kpad, kk,
                                         (float)(ss / (xs * xs)), 0.f, 0.f};
@@ -661,28 +667,44 @@ hipError_t iterate(const OrthSizes& z, const dte_newton_schulz& ns, const Bounds
         u.nj = (int32_t)z.rpad;
         u.steps = (int32_t)(z.kpad / 64);
         u.split = 1;
-        u.batch = (int32_t)z.batch;
+        u.batch = (int32_t)batch;
+        const bool last = k + 1 == ns.steps;
+        const double next = last ? 1.0 : fp16_scale(bd.sigma[k + 1]);
         const LinearTerm lin{b.hi[k & 1], b.lo, b.diag, z.cpad, n, z.kpad,
-                             (float)ns.coefficients[k][0], (float)(1.0 / xs),
-                             (float)(1.0 / (bs * xs))};
-        if (k + 1 == ns.steps) return last_product<kWide>(u, lin, z, o, st);
-        xs = fp16_scale(bd.sigma[k + 1]);
-        const typename NextEpi<kWide>::Args en{lin, b.hi[(k + 1) & 1], b.lo, (float)xs};
+                             (float)ns.coefficients[k][0], (float)(next / xs),
+                             (float)(next / (bs * xs))};
+        if (last) return last_product<kWide>(u, lin, z, o, st);
+        xs = next;
+        const typename NextEpi<kWide>::Args en{lin, b.hi[(k + 1) & 1], b.lo};
         err = product<kA, pr::kK, NextEpi<kWide>>(u, en, st);
         if (err != hipSuccess) return err;
     }
     return hipSuccess;
 }
 
-hipError_t orthogonalise(const Source& src, const OrthSizes& z, const dte_newton_schulz& ns,
-                         const Bounds& bd, const Result& o, const OrthBuffers& b, hipStream_t st)
+// Matrices b0 .. b0 + batch of the call.
+hipError_t group(Source src, const OrthSizes& z, int64_t b0, int64_t batch,
+                 const dte_newton_schulz& ns, const Bounds& bd, Result o, const OrthBuffers& b,
+                 hipStream_t st)
 {
+    const int64_t n = z.rows * z.cols;
+    Muon muon{};
+    if (src.momentum) {
+        src.momentum += b0 * n;
+        src.g += b0 * n;
+        muon = *o.muon;
+        muon.p += b0 * n;
+        o.muon = &muon;
+    } else {
+        src.x = (const char*)src.x + b0 * src.stride * (src.bf16 ? 2 : 4);
+    }
+    o.out += b0 * o.stride;
     const int32_t parts = (int32_t)norm_parts(z);
-    const dim3 block(256), ngrid((unsigned)parts, (unsigned)z.batch);
+    const dim3 block(256), ngrid((unsigned)parts, (unsigned)batch);
     int64_t blocks = div_up(z.rpad * z.cpad / 4, 256);
-    const int64_t most = div_up(8192, z.batch);
+    const int64_t most = div_up(8192, batch);
     if (blocks > most) blocks = most;
-    const dim3 xgrid((unsigned)blocks, (unsigned)z.batch);
+    const dim3 xgrid((unsigned)blocks, (unsigned)batch);
     const int32_t rows = (int32_t)z.rows, cols = (int32_t)z.cols;
     bool vec = cols % 4 == 0;
     if (src.momentum)
@@ -704,7 +726,19 @@ hipError_t orthogonalise(const Source& src, const OrthSizes& z, const dte_newton
     }
     const hipError_t err = hipGetLastError();
     if (err != hipSuccess) return err;
-    return z.wide ? iterate<true>(z, ns, bd, b, o, st) : iterate<false>(z, ns, bd, b, o, st);
+    return z.wide ? iterate<true>(z, batch, ns, bd, b, o, st)
+                  : iterate<false>(z, batch, ns, bd, b, o, st);
+}
+
+hipError_t orthogonalise(const Source& src, const OrthSizes& z, const dte_newton_schulz& ns,
+                         const Bounds& bd, const Result& o, const OrthBuffers& b, hipStream_t st)
+{
+    for (int64_t b0 = 0; b0 < z.batch; b0 += z.group) {
+        const int64_t batch = z.batch - b0 < z.group ? z.batch - b0 : z.group;
+        const hipError_t err = group(src, z, b0, batch, ns, bd, o, b, st);
+        if (err != hipSuccess) return err;
+    }
+    return hipSuccess;
 }
 
 }  // namespace

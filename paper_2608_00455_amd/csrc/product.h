@@ -333,15 +333,16 @@ __device__ __forceinline__ void tile_product(const ProductArgs& p, const TileAt&
         lb.advance(p.b, j0, s);
     };
     // steps s0 and s0 + 1 (the last one again where there is no more: what is
-    // loaded is then not used)
+    // loaded is then not used); the first has landed when only the second's
+    // loads are outstanding
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) load(lds, i);
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
     if (s0 + 1 < s1) advance(s0 + 1);
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) load(lds + kStage, i);
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLoads) : "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
 
     s16x8 a[S::FI], b[2][S::FJ];
 #pragma unroll
