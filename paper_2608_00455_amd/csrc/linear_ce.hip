@@ -420,16 +420,13 @@ struct Sizes {
 
 int tile_i(ShapeKind k) { return k == kMedium ? 128 : 256; }
 
-// Tile shape of a product with ni x nj outputs.  256 x 256 tiles read each
-// operand from LDS half as often as 128 x 128 ones, which is worth having once
-// there are tiles for most of the CUs; few j take the thin shapes, which do
-// not multiply rows that are not there.
+// Tile shape of a product with ni x nj outputs: few j take the thin shapes,
+// which do not multiply rows that are not there.
 ShapeKind shape_for(int64_t ni, int64_t nj, int cus)
 {
     if (nj <= 32) return kThin32;
     if (nj <= 64) return kThin64;
-    const int64_t large = div_up(ni, 256) * div_up(nj, 256);
-    return large * 4 >= (int64_t)cus * 3 ? kLarge : kMedium;
+    return pr::tiles_for(ni, nj, 1, false, false, cus) == pr::Tiles::kLarge ? kLarge : kMedium;
 }
 
 constexpr int64_t kPieceBytes = (int64_t)256 << 20;   // of G

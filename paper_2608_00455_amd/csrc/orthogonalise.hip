@@ -521,6 +521,11 @@ struct OrthSizes {
     bool wide;
 };
 
+// Workspace of one matrix; and of all that are worked on together.  (Smaller
+// groups, whose work would stay in the 256 MiB last-level cache, leave the
+// products' last rounds emptier than they win: 128 matrices of 768 x 2048 in
+// groups of 128 / 64 / 32 / 16 take 4.7 / 5.0 / 5.1 / 5.2 ms.)
+constexpr int64_t kGroupBytes = (int64_t)4 << 30;
 int64_t work_bytes(const OrthSizes& z)
 {
     return 6 * z.rpad * z.cpad + 4 * z.kpad * z.kpad;
@@ -538,9 +543,11 @@ bool orth_sizes(int64_t batch, int64_t rows, int64_t cols, OrthSizes* z)
     z->cpad = round_up(cols, 64);
     z->wide = rows <= cols;
     z->kpad = z->wide ? z->rpad : z->cpad;
+    // as many as 4 GiB hold, or one
     z->group = batch;
-    if (getenv("DTE_G")) z->group = atoi(getenv("DTE_G"));
-    if (z->group > batch) z->group = batch;
+    const int64_t bytes = work_bytes(*z);
+    if (bytes > 0 && z->group > kGroupBytes / bytes) z->group = kGroupBytes / bytes;
+    if (z->group < 1) z->group = 1;
     return true;
 }
 
@@ -574,26 +581,18 @@ int64_t carve(const OrthSizes& z, void* ws, OrthBuffers* b)
     return c.used;
 }
 
-// Tile shape by the rounds that the blocks take: a round of 256 x 256 tiles
-// (one per CU) does four units of work, one of 128 x 128 tiles (two per CU)
-// two units at nine tenths of the rate.
-bool large_tiles(int64_t ni, int64_t nj, int64_t batch, bool symmetric, int cus)
-{
-    auto rounds = [&](int64_t t, int64_t slots) {
-        const int64_t a = div_up(ni, t), b = div_up(nj, t);
-        return div_up(batch * (symmetric ? a * (a + 1) / 2 : a * b), slots);
-    };
-    return rounds(256, cus) * 4.0 <= rounds(128, 2 * cus) * 2.2;
-}
-
 template <pr::Layout kA, pr::Layout kB, class Epi>
-hipError_t product(pr::ProductArgs p, const typename Epi::Args& e, hipStream_t st)
+hipError_t product(const pr::ProductArgs& p, const typename Epi::Args& e, hipStream_t st)
 {
-    if (getenv("DTE_M") && p.symmetric == 0) return pr::launch_product<pr::Medium, true, kA, kB, Epi>(p, e, st);
-    if (getenv("DTE_MS") && p.symmetric != 0) return pr::launch_product<pr::Medium, true, kA, kB, Epi>(p, e, st);
-    return large_tiles(p.ni, p.nj, p.batch, p.symmetric != 0, device_cus())
-               ? pr::launch_product<pr::Large, true, kA, kB, Epi>(p, e, st)
-               : pr::launch_product<pr::Medium, true, kA, kB, Epi>(p, e, st);
+    constexpr bool kMiddle = kA == pr::kK && kB == pr::kK;
+    switch (pr::tiles_for(p.ni, p.nj, p.batch, p.symmetric != 0, kMiddle, device_cus())) {
+    case pr::Tiles::kLarge: return pr::launch_product<pr::Large, true, kA, kB, Epi>(p, e, st);
+    case pr::Tiles::kMiddle:
+        if constexpr (kMiddle) return pr::launch_product<pr::Middle, true, kA, kB, Epi>(p, e, st);
+        return hipErrorInvalidValue;       // (not chosen)
+    case pr::Tiles::kMedium: break;
+    }
+    return pr::launch_product<pr::Medium, true, kA, kB, Epi>(p, e, st);
 }
 
 struct Muon {

@@ -286,8 +286,10 @@ struct Shape {
     static constexpr int FI = kTI / kWI / 16, FJ = kTJ / kWJ / 16;
     static constexpr uint32_t kStageBytes = (kTI + kTJ) * kStepK * 2;
     static constexpr uint32_t kLds = 2 * kStageBytes;
+    static constexpr int kMinWaves = kThreads > 512 ? 3 : 2;   // per SIMD
 };
 typedef Shape<256, 256, 2, 4> Large;     // one block per CU
+typedef Shape<192, 192, 3, 4> Middle;    // one block per CU, k-contiguous operands
 typedef Shape<128, 128, 2, 2> Medium;    // two blocks per CU
 typedef Shape<256, 64, 4, 1> Thin64;     // few j: the i operand streams past
 typedef Shape<256, 32, 4, 1> Thin32;
@@ -480,7 +482,7 @@ __device__ __forceinline__ void for_rows(const LanePos<S>& pos, f32x4 (&acc)[S::
 
 // Epi::run(args, product, at, pos, acc) takes the sums.
 template <class S, bool kF16, Layout kA, Layout kB, class Epi>
-__global__ __launch_bounds__(S::kThreads, 2) void product_kernel(ProductArgs p,
+__global__ __launch_bounds__(S::kThreads, S::kMinWaves) void product_kernel(ProductArgs p,
                                                                  typename Epi::Args e,
                                                                  int32_t per_matrix)
 {
@@ -521,6 +523,29 @@ hipError_t launch_product(ProductArgs p, const typename Epi::Args& e, hipStream_
     hipLaunchKernelGGL((product_kernel<S, kF16, kA, kB, Epi>), dim3((unsigned)blocks),
                        dim3(S::kThreads), S::kLds, stream, p, e, (int32_t)(tiles * p.split));
     return hipGetLastError();
+}
+
+// Which tile shape a product of ni x nj outputs takes.  Blocks run in rounds
+// of what the chip holds; a round takes, relative to 256 x 256 tiles (105 us
+// at K 4096), 0.65 with 192 x 192 tiles (68 us) and 0.62 with 128 x 128 ones,
+// two per CU (65 us; 0.4 with one per CU).  So large tiles are worth having
+// unless they leave much of the last round empty: the 136 tiles of a symmetric
+// 4096 x 4096 product fill half of one (97 us), its 253 middle ones all of
+// theirs (69 us).
+enum class Tiles { kLarge, kMiddle, kMedium };
+inline Tiles tiles_for(int64_t ni, int64_t nj, int64_t batch, bool symmetric, bool middle, int cus)
+{
+    auto blocks = [&](int64_t t) {
+        const int64_t a = (ni + t - 1) / t, b = (nj + t - 1) / t;
+        return batch * (symmetric ? a * (a + 1) / 2 : a * b);
+    };
+    auto rounds = [&](int64_t t, int64_t slots) {
+        return (double)((blocks(t) + slots - 1) / slots);
+    };
+    const double large = rounds(256, cus), mid = middle ? rounds(192, cus) * 0.65 : 1e30;
+    const double medium = blocks(128) <= cus ? 0.4 : rounds(128, 2 * cus) * 0.62;
+    if (large <= mid && large <= medium) return Tiles::kLarge;
+    return mid <= medium ? Tiles::kMiddle : Tiles::kMedium;
 }
 
 }  // namespace pr
