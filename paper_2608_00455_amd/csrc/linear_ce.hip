@@ -139,6 +139,209 @@ struct StatsEpi {
     }
 };
 
+// The same for at most 16 kJ <= 64 tokens, where all of the time goes into
+// reading the weight once: no LDS in its way.  A wave takes 16 vocabulary rows
+// at a time and loads them straight into the registers of the matrix
+// instructions' row operand (16 bytes per lane: 64 consecutive bytes of 16
+// rows), kFlight loads in flight, each replaced as soon as it is used, over
+// the ends of rows too.  The tokens lie in LDS, as much of their dim as fits
+// (kPhase values); where that is not all, the sums of kRowGroups groups of rows wait
+// in registers for the next phase.  Statistics stay in registers until the
+// block ends: one pair per block and token.  Vocabulary 151936, 1 token of dim
+// 4096: 290 us with the tiles above.
+constexpr int kStreamWaves = 8, kFlight = 16;
+constexpr int kStreamLds = 128 * 1024;
+
+struct StreamArgs {
+    const uint16_t* w;
+    const uint16_t* h;     // [64][dpad]
+    const int64_t* targets;
+    float2* part;
+    float* target_z;
+    int64_t ld, dpad, tpad, v0;
+    int32_t n, tokens, part0, phase;   // rows; phase: of dim, a multiple of 64
+    float scale;
+};
+
+template <int kJ, int kRowGroups>
+__global__ __launch_bounds__(kStreamWaves * 64, 2) void stream_stats_kernel(StreamArgs a)
+{
+#ifdef __HIP_DEVICE_COMPILE__
+    using pr::s16x8;
+    const int lane = threadIdx.x & 63, j = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t lds = pr::lds_base();
+    const int32_t groups = (a.n + 15) / 16, per = (groups + gridDim.x - 1) / gridDim.x;
+    const int32_t first = blockIdx.x * per, last = min(groups, first + per);
+    float m[kJ], sum[kJ];
+#pragma unroll
+    for (int t = 0; t < kJ; ++t) {
+        m[t] = -INFINITY;
+        sum[t] = 0.f;
+    }
+    int64_t target[kJ];
+#pragma unroll
+    for (int t = 0; t < kJ; ++t)
+        target[t] = t * 16 + j < a.tokens ? a.targets[t * 16 + j] - a.v0 : -1;
+
+    const int32_t phases = (int32_t)((a.dpad + a.phase - 1) / a.phase);
+    // row of this lane in group q (the last row again beyond the end)
+    auto row = [&](int32_t q) {
+        const int64_t r = (int64_t)q * 16 + j;
+        return a.w + (r < a.n ? r : a.n - 1) * a.ld + g * 8;
+    };
+    s16x8 w[kFlight];
+    const uint16_t* p = nullptr;
+    for (int32_t base = first; base < last; base += kStreamWaves * kRowGroups) {
+        f32x4 acc[kRowGroups][kJ];
+#pragma unroll
+        for (int q = 0; q < kRowGroups; ++q)
+#pragma unroll
+            for (int t = 0; t < kJ; ++t) acc[q][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int32_t ph = 0; ph < phases; ++ph) {
+            // blocks begin with different phases: the halves of 4 KB rows lie
+            // in different memory channels
+            const int32_t k0 = (ph + blockIdx.x) % phases * a.phase;
+            const int32_t width = (int32_t)(a.dpad - k0 < a.phase ? a.dpad - k0 : a.phase);
+            if (phases > 1 || base == first) {
+                // tokens [16 kJ][width] to LDS, 16-byte chunk c of a row at c ^ (row & 7)
+                __syncthreads();
+                const int32_t chunks = width / 8;
+                for (int32_t x = threadIdx.x; x < 16 * kJ * chunks; x += kStreamWaves * 64) {
+                    const int32_t r = x / chunks, c = x - r * chunks;
+                    *(DTE_LDS(s16x8)*)(uintptr_t)(lds + (r * chunks + (c ^ (r & 7))) * 16) =
+                        *(const s16x8*)(a.h + r * a.dpad + k0 + c * 8);
+                }
+                __syncthreads();
+            }
+            const uint32_t rows = lds + j * width * 2;
+            const int32_t q0 = base + wave;
+            if (phases > 1 || base == first) {
+                p = row(q0 < last ? q0 : last - 1) + k0;
+#pragma unroll
+                for (int i = 0; i < kFlight; ++i)
+                    w[i] = *(const s16x8*)(p + (i * 32 < width ? i * 32 : 0));
+            }
+#pragma unroll
+            for (int q = 0; q < kRowGroups; ++q) {
+                const int32_t mine = q0 + q * kStreamWaves;
+                if (mine >= last) break;
+                // the rows after these, or one address again and again
+                const int32_t nq = mine + kStreamWaves;
+                const bool more = nq < last && (q + 1 < kRowGroups || phases == 1);
+                const uint16_t* np = row(more ? nq : mine) + k0;
+                for (int32_t k = 0; k < width; k += 32 * kFlight) {
+                    const bool end = k + 32 * kFlight >= width;
+                    const uint16_t* from = end ? np : p + k + 32 * kFlight;
+                    const int32_t room = !end ? width - k - 32 * kFlight : more ? width : 0;
+#pragma unroll
+                    for (int i = 0; i < kFlight; ++i) {
+                        if (k + 32 * i < width) {
+                            const int32_t c = (k >> 3) + i * 4 + g;
+#pragma unroll
+                            for (int t = 0; t < kJ; ++t) {
+                                const s16x8 h = *(DTE_LDS(s16x8)*)(uintptr_t)(
+                                    rows + t * 32 * width + ((c ^ (j & 7)) * 16));
+                                acc[q][t] = pr::mfma<false>(w[i], h, acc[q][t]);
+                            }
+                        }
+                        w[i] = *(const s16x8*)(from + (32 * i < room ? 32 * i : 0));
+                    }
+                }
+                p = np;
+            }
+        }
+#pragma unroll
+        for (int q = 0; q < kRowGroups; ++q) {
+            const int32_t mine = base + wave + q * kStreamWaves;
+            if (mine >= last) break;
+            const int64_t r0 = (int64_t)mine * 16 + 4 * g;
+#pragma unroll
+            for (int t = 0; t < kJ; ++t) {
+                float top = m[t];
+                f32x4 z = acc[q][t] * a.scale;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    if (target[t] == r0 + r) a.target_z[t * 16 + j] = z[r];
+                    if (r0 + r >= a.n) z[r] = -INFINITY;
+                    top = fmaxf(top, z[r]);
+                }
+                const float o = top == -INFINITY ? 0.f : top;
+                sum[t] *= __builtin_amdgcn_exp2f((m[t] - o) * kLog2e);
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    sum[t] += __builtin_amdgcn_exp2f((z[r] - o) * kLog2e);
+                m[t] = top;
+            }
+        }
+    }
+    // across the lanes of a token, then the waves
+    __syncthreads();
+    float2* s_pair = (float2*)pr::s_dynamic;     // [wave][16 kJ]
+#pragma unroll
+    for (int t = 0; t < kJ; ++t) {
+#pragma unroll
+        for (int d = 16; d < 64; d <<= 1) {
+            const float m2 = __shfl_xor(m[t], d), s2 = __shfl_xor(sum[t], d);
+            const float top = fmaxf(m[t], m2), o = top == -INFINITY ? 0.f : top;
+            sum[t] = sum[t] * __builtin_amdgcn_exp2f((m[t] - o) * kLog2e) +
+                     s2 * __builtin_amdgcn_exp2f((m2 - o) * kLog2e);
+            m[t] = top;
+        }
+        if (g == 0) s_pair[wave * 16 * kJ + t * 16 + j] = make_float2(m[t], sum[t]);
+    }
+    __syncthreads();
+    if (threadIdx.x < 16 * kJ && threadIdx.x < a.tpad) {
+        float2 x = s_pair[threadIdx.x];
+        for (int w = 1; w < kStreamWaves; ++w) {
+            const float2 y = s_pair[w * 16 * kJ + threadIdx.x];
+            const float top = fmaxf(x.x, y.x), o = top == -INFINITY ? 0.f : top;
+            x.y = x.y * __builtin_amdgcn_exp2f((x.x - o) * kLog2e) +
+                  y.y * __builtin_amdgcn_exp2f((y.x - o) * kLog2e);
+            x.x = top;
+        }
+        a.part[(int64_t)(a.part0 + blockIdx.x) * a.tpad + threadIdx.x] = x;
+    }
+#endif
+}
+
+// Blocks of the streaming kernel: one per CU, or one per kStreamWaves groups of rows.
+int32_t stream_blocks(int64_t n, int cus)
+{
+    const int64_t b = div_up(div_up(n, 16), kStreamWaves);
+    return (int32_t)(b < cus ? b : cus);
+}
+
+template <int kJ, int kRowGroups>
+hipError_t launch_stream(const StreamArgs& a, int32_t blocks, hipStream_t st)
+{
+    const hipError_t err = pr::allow_lds((const void*)stream_stats_kernel<kJ, kRowGroups>,
+                                         kStreamLds);
+    if (err != hipSuccess) return err;
+    stream_stats_kernel<kJ, kRowGroups>
+        <<<dim3((unsigned)blocks), dim3(kStreamWaves * 64), kStreamLds, st>>>(a);
+    return hipGetLastError();
+}
+
+hipError_t stream_stats(StreamArgs a, int32_t blocks, hipStream_t st)
+{
+    const int kj = a.tokens <= 16 ? 1 : a.tokens <= 32 ? 2 : 4;
+    const int64_t most = kStreamLds / (16 * kj * 2);   // of dim, in LDS at once
+    a.phase = (int32_t)(a.dpad < most ? a.dpad : most);
+    if (a.dpad <= most) {
+        switch (kj) {
+        case 1: return launch_stream<1, 1>(a, blocks, st);
+        case 2: return launch_stream<2, 1>(a, blocks, st);
+        default: return launch_stream<4, 1>(a, blocks, st);
+        }
+    }
+    switch (kj) {
+    case 1: return launch_stream<1, 5>(a, blocks, st);
+    case 2: return launch_stream<2, 5>(a, blocks, st);
+    default: return launch_stream<4, 5>(a, blocks, st);
+    }
+}
+
 // Joins the pairs of a token: 16 tokens per block, 16 lanes per token.
 __global__ __launch_bounds__(256) void join_stats_kernel(const float2* part, int64_t tpad,
                                                          int32_t parts, const float* target_z,
@@ -406,7 +609,7 @@ __global__ __launch_bounds__(256) void hidden_grad_kernel(const float* part, int
 
 // ---- the plan of a call ---------------------------------------------------------
 
-enum ShapeKind { kLarge, kMedium, kThin64, kThin32 };
+enum ShapeKind { kLarge, kMedium, kDeep, kThin64, kThin32 };
 
 struct Sizes {
     int64_t T, V, d, tpad, dpad;
@@ -416,9 +619,10 @@ struct Sizes {
     int32_t terms, split;
     int64_t parts;         // tile rows of the forward statistics
     ShapeKind logits, hid, wgt;
+    bool stream;           // forward: few tokens
 };
 
-int tile_i(ShapeKind k) { return k == kMedium ? 128 : 256; }
+int tile_i(ShapeKind k) { return k == kMedium || k == kDeep ? 128 : 256; }
 
 // Tile shape of a product with ni x nj outputs: few j take the thin shapes,
 // which do not multiply rows that are not there.
@@ -426,7 +630,11 @@ ShapeKind shape_for(int64_t ni, int64_t nj, int cus)
 {
     if (nj <= 32) return kThin32;
     if (nj <= 64) return kThin64;
-    return pr::tiles_for(ni, nj, 1, false, false, cus) == pr::Tiles::kLarge ? kLarge : kMedium;
+    switch (pr::tiles_for(ni, nj, 1, false, false, cus)) {
+    case pr::Tiles::kLarge: return kLarge;
+    case pr::Tiles::kDeep: return kDeep;
+    default: return kMedium;
+    }
 }
 
 constexpr int64_t kPieceBytes = (int64_t)256 << 20;   // of G
@@ -458,7 +666,10 @@ bool sizes_of(const dte_linear_ce* c, bool backward, int32_t grad_type, Sizes* s
             s->piece = rows < 256 ? 256 : rows;
             if (s->piece > s->V) s->piece = s->V;
         }
-        s->parts = div_up(s->V, s->piece) * div_up(s->piece, tile_i(s->logits));
+        s->stream = s->T <= 64;
+        s->parts = div_up(s->V, s->piece) *
+                   (s->stream ? stream_blocks(s->piece, cus)
+                              : div_up(s->piece, tile_i(s->logits)));
         return true;
     }
     int64_t cols = s->tpad ? kPieceBytes / (s->tpad * 2 * s->terms) / 256 * 256 : 256;
@@ -474,7 +685,7 @@ bool sizes_of(const dte_linear_ce* c, bool backward, int32_t grad_type, Sizes* s
     s->wgt = shape_for(s->d, s->piece > 64 ? s->piece : 65, cus);
     // few tiles of grad_hidden: share each tile's vocabulary rows among blocks
     const int64_t ti = tile_i(s->hid);
-    const int64_t tj = s->hid == kLarge ? 256 : s->hid == kMedium ? 128 : s->hid == kThin64 ? 64 : 32;
+    const int64_t tj = s->hid == kLarge ? 256 : tile_i(s->hid) == 128 ? 128 : s->hid == kThin64 ? 64 : 32;
     const int64_t tiles = div_up(s->d, ti) * div_up(s->T > 0 ? s->T : 1, tj);
     const int64_t slots = s->hid == kLarge ? cus : 2 * cus;
     int64_t split = slots / tiles;
@@ -517,6 +728,7 @@ hipError_t product(ShapeKind k, const pr::ProductArgs& p, const typename Epi::Ar
     switch (k) {
     case kLarge: return pr::launch_product<pr::Large, false, kA, kB, Epi>(p, e, st);
     case kMedium: return pr::launch_product<pr::Medium, false, kA, kB, Epi>(p, e, st);
+    case kDeep: return pr::launch_product<pr::Deep, false, kA, kB, Epi>(p, e, st);
     default: break;
     }
     if constexpr (kB == pr::kK) {      // the thin shapes take a k-contiguous j operand only
@@ -576,6 +788,14 @@ dte_status forward(const dte_linear_ce* c, const Sizes& s, const Buffers& b, flo
         const int64_t n = s.V - v0 < s.piece ? s.V - v0 : s.piece;
         WeightRows w;
         DTE_TRY(weight_rows(c, s, b, v0, n, st, &w));
+        if (s.stream) {
+            const int32_t blocks = stream_blocks(n, device_cus());
+            const StreamArgs a{w.p, b.h, c->targets, b.part, b.target_z, w.ld, s.dpad, s.tpad, v0,
+                               (int32_t)n, (int32_t)s.T, part0, 0, c->scale};
+            DTE_TRY(stream_stats(a, blocks, st));
+            part0 += blocks;
+            continue;
+        }
         const pr::ProductArgs p = logits_product(s, b, w, n);
         const StatsEpi::Args e{c->targets, b.part, b.target_z, s.tpad, (int32_t)s.T, s.V, v0,
                                part0,      c->scale};

@@ -590,6 +590,7 @@ hipError_t product(const pr::ProductArgs& p, const typename Epi::Args& e, hipStr
     case pr::Tiles::kMiddle:
         if constexpr (kMiddle) return pr::launch_product<pr::Middle, true, kA, kB, Epi>(p, e, st);
         return hipErrorInvalidValue;       // (not chosen)
+    case pr::Tiles::kDeep: return pr::launch_product<pr::Deep, true, kA, kB, Epi>(p, e, st);
     case pr::Tiles::kMedium: break;
     }
     return pr::launch_product<pr::Medium, true, kA, kB, Epi>(p, e, st);

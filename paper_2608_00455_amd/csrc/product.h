@@ -9,7 +9,7 @@
 //
 // A block owns a tile of TI x TJ outputs and walks k in steps of 64.  Each
 // step's operand tiles go straight from memory to LDS (16-byte buffer loads
-// with an LDS destination), into one of two buffers.  A wave's outputs stay in
+// with an LDS destination), into one of two to four buffers.  A wave's outputs stay in
 // registers; it reads fragments of 16 rows x 32 k and issues
 // v_mfma_f32_16x16x32.  The i side is the instruction's row operand, so a lane
 // ends up with four consecutive i of one j: 8- or 16-byte stores, and
@@ -19,8 +19,8 @@
 // first half (32 k) of step s is multiplied, the fragments of the second half
 // are read, after which nobody reads step s's buffer any more; the barrier
 // makes that known (and that step s + 1 has landed), and while the second half
-// is multiplied the loads of step s + 2 go into that buffer and the fragments
-// of step s + 1's first half are read.  Reads and loads are issued one row of
+// is multiplied the loads of the next step that fits go into that buffer and
+// the fragments of step s + 1's first half are read.  Reads and loads are issued one row of
 // matrix instructions apart, or they would fill their queues and hold the
 // matrix instructions up.  8192^3 in BF16, TFLOP/s, k-contiguous operands /
 // one row-contiguous / both: 1160 / 1165 / 1155 (a library product with
@@ -278,21 +278,23 @@ __device__ __forceinline__ TileAt tile_of(const ProductArgs& p, int32_t per_matr
     return at;
 }
 
-// Tile shapes: kWI x kWJ waves, each with (TI / kWI) x (TJ / kWJ) outputs.
-template <int kTI, int kTJ, int kWI_, int kWJ_>
+// Tile shapes: kWI x kWJ waves, each with (TI / kWI) x (TJ / kWJ) outputs;
+// kStages buffers, so kStages - 1 steps of loads in flight.
+template <int kTI, int kTJ, int kWI_, int kWJ_, int kStages_ = 2>
 struct Shape {
-    static constexpr int TI = kTI, TJ = kTJ, kWI = kWI_, kWJ = kWJ_;
+    static constexpr int TI = kTI, TJ = kTJ, kWI = kWI_, kWJ = kWJ_, kStages = kStages_;
     static constexpr int kThreads = kWI * kWJ * 64;
     static constexpr int FI = kTI / kWI / 16, FJ = kTJ / kWJ / 16;
     static constexpr uint32_t kStageBytes = (kTI + kTJ) * kStepK * 2;
-    static constexpr uint32_t kLds = 2 * kStageBytes;
+    static constexpr uint32_t kLds = kStages * kStageBytes;
     static constexpr int kMinWaves = kThreads > 512 ? 3 : 2;   // per SIMD
 };
-typedef Shape<256, 256, 2, 4> Large;     // one block per CU
-typedef Shape<192, 192, 3, 4> Middle;    // one block per CU, k-contiguous operands
-typedef Shape<128, 128, 2, 2> Medium;    // two blocks per CU
-typedef Shape<256, 64, 4, 1> Thin64;     // few j: the i operand streams past
-typedef Shape<256, 32, 4, 1> Thin32;
+typedef Shape<256, 256, 2, 4> Large;       // one block per CU
+typedef Shape<192, 192, 3, 4, 3> Middle;   // one block per CU, k-contiguous operands
+typedef Shape<128, 128, 2, 2> Medium;      // two blocks per CU
+typedef Shape<128, 128, 2, 2, 4> Deep;     // one block per CU
+typedef Shape<256, 64, 4, 1, 4> Thin64;    // few j: the i operand streams past
+typedef Shape<256, 32, 4, 1, 4> Thin32;
 
 // The k loop.  On return the block's waves have left the loop together and no
 // load to LDS is in flight, so the epilogue may use all of the LDS.
@@ -334,15 +336,16 @@ __device__ __forceinline__ void tile_product(const ProductArgs& p, const TileAt&
         la.advance(p.a, i0, s);
         lb.advance(p.b, j0, s);
     };
-    // steps s0 and s0 + 1 (the last one again where there is no more: what is
-    // loaded is then not used); the first has landed when only the second's
-    // loads are outstanding
+    // The first kStages steps (the last one again where there is no more: what
+    // is loaded then is not used).  Loads return in order: the first step has
+    // landed when only the others' loads are outstanding.
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) load(lds, i);
-    if (s0 + 1 < s1) advance(s0 + 1);
+    for (int t = 0; t < S::kStages; ++t) {
+        if (t > 0 && s0 + t < s1) advance(s0 + t);
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) load(lds + kStage, i);
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLoads) : "memory");
+        for (int i = 0; i < kLoads; ++i) load(lds + t * kStage, i);
+    }
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"((S::kStages - 1) * kLoads) : "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
 
@@ -351,10 +354,10 @@ __device__ __forceinline__ void tile_product(const ProductArgs& p, const TileAt&
     for (int j = 0; j < S::FJ; ++j) b[0][j] = fb.read(lds + kBAt, j, 0);
 #pragma unroll
     for (int i = 0; i < S::FI; ++i) a[i] = fa.read(lds, i, 0);
+    uint32_t cur = lds;
     for (int32_t s = s0; s < s1; ++s) {
-        const uint32_t odd = (s - s0) & 1;
-        const uint32_t cur = lds + (odd ? kStage : 0), next = lds + (odd ? 0 : kStage);
-        if (s + 2 < s1) advance(s + 2);
+        const uint32_t next = cur + kStage == lds + S::kLds ? lds : cur + kStage;
+        if (s + S::kStages < s1) advance(s + S::kStages);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int i = 0; i < S::FI; ++i) {
@@ -368,7 +371,8 @@ __device__ __forceinline__ void tile_product(const ProductArgs& p, const TileAt&
         }
         // step s + 1 has landed for every wave, and every wave is done reading
         // step s's buffer
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((S::kStages - 2) * kLoads)
+                     : "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         __builtin_amdgcn_sched_barrier(0);
@@ -384,6 +388,7 @@ __device__ __forceinline__ void tile_product(const ProductArgs& p, const TileAt&
             a[i] = t;
             __builtin_amdgcn_sched_barrier(0);
         }
+        cur = next;
     }
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
@@ -495,6 +500,14 @@ __global__ __launch_bounds__(S::kThreads, S::kMinWaves) void product_kernel(Prod
 #endif
 }
 
+// More dynamic LDS than the default limit of 64 KiB: an attribute of the
+// function (a call of about a microsecond that changes nothing when repeated).
+inline hipError_t allow_lds(const void* kernel, int bytes)
+{
+    if (bytes <= 65536) return hipSuccess;
+    return hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+}
+
 template <class S, bool kF16, Layout kA, Layout kB, class Epi>
 hipError_t launch_product(ProductArgs p, const typename Epi::Args& e, hipStream_t stream)
 {
@@ -505,21 +518,9 @@ hipError_t launch_product(ProductArgs p, const typename Epi::Args& e, hipStream_
     const int64_t blocks = tiles * p.split * p.batch;
     if (blocks <= 0) return hipSuccess;
     if (blocks > 0x7fffffff) return hipErrorInvalidValue;
-    const void* k = (const void*)product_kernel<S, kF16, kA, kB, Epi>;
-    if (S::kLds > 65536) {
-        // more dynamic LDS than the default limit: an attribute of the
-        // function, set once per device
-        static std::atomic<uint64_t> done{0};
-        int dev = 0;
-        hipError_t err = hipGetDevice(&dev);
-        if (err != hipSuccess) return err;
-        const uint64_t bit = dev < 64 ? 1ull << dev : 0;
-        if (!(done.load(std::memory_order_relaxed) & bit) || !bit) {
-            err = hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, S::kLds);
-            if (err != hipSuccess) return err;
-            done.fetch_or(bit, std::memory_order_relaxed);
-        }
-    }
+    const hipError_t err =
+        allow_lds((const void*)product_kernel<S, kF16, kA, kB, Epi>, S::kLds);
+    if (err != hipSuccess) return err;
     hipLaunchKernelGGL((product_kernel<S, kF16, kA, kB, Epi>), dim3((unsigned)blocks),
                        dim3(S::kThreads), S::kLds, stream, p, e, (int32_t)(tiles * p.split));
     return hipGetLastError();
@@ -532,7 +533,7 @@ hipError_t launch_product(ProductArgs p, const typename Epi::Args& e, hipStream_
 // unless they leave much of the last round empty: the 136 tiles of a symmetric
 // 4096 x 4096 product fill half of one (97 us), its 253 middle ones all of
 // theirs (69 us).
-enum class Tiles { kLarge, kMiddle, kMedium };
+enum class Tiles { kLarge, kMiddle, kMedium, kDeep };
 inline Tiles tiles_for(int64_t ni, int64_t nj, int64_t batch, bool symmetric, bool middle, int cus)
 {
     auto blocks = [&](int64_t t) {
@@ -545,7 +546,8 @@ inline Tiles tiles_for(int64_t ni, int64_t nj, int64_t batch, bool symmetric, bo
     const double large = rounds(256, cus), mid = middle ? rounds(192, cus) * 0.65 : 1e30;
     const double medium = blocks(128) <= cus ? 0.4 : rounds(128, 2 * cus) * 0.62;
     if (large <= mid && large <= medium) return Tiles::kLarge;
-    return mid <= medium ? Tiles::kMiddle : Tiles::kMedium;
+    if (mid <= medium) return Tiles::kMiddle;
+    return blocks(128) <= cus ? Tiles::kDeep : Tiles::kMedium;
 }
 
 }  // namespace pr
