@@ -22,6 +22,8 @@
 #include <hip/hip_runtime.h>
 
 #include <cmath>
+#include <numeric>
+#include <type_traits>
 
 #include "abi_guard.h"
 #include "product.h"
@@ -342,35 +344,43 @@ hipError_t stream_stats(StreamArgs a, int32_t blocks, hipStream_t st)
     }
 }
 
-// Joins the pairs of a token: 16 tokens per block, 16 lanes per token.
+// Joins the pairs of a token: `tok` tokens per block, 256 / tok lanes each.
+__device__ __forceinline__ float2 join(float2 a, float2 b)
+{
+    const float m = fmaxf(a.x, b.x), o = m == -INFINITY ? 0.f : m;
+    return make_float2(m, a.y * __builtin_amdgcn_exp2f((a.x - o) * kLog2e) +
+                              b.y * __builtin_amdgcn_exp2f((b.x - o) * kLog2e));
+}
 __global__ __launch_bounds__(256) void join_stats_kernel(const float2* part, int64_t tpad,
-                                                         int32_t parts, const float* target_z,
+                                                         int32_t parts, int32_t tok,
+                                                         const float* target_z,
                                                          const int64_t* targets, int64_t vocab,
                                                          int32_t tokens, float* loss, float* lse)
 {
-    __shared__ float2 s[16][17];
-    const int x = threadIdx.x & 15, y = threadIdx.x >> 4;
-    const int64_t t = (int64_t)blockIdx.x * 16 + x;
-    float m = -INFINITY, sum = 0.f;
-    if (t < tokens)
-        for (int32_t k = y; k < parts; k += 16) {
-            const float2 b = part[(int64_t)k * tpad + t];
-            const float n = fmaxf(m, b.x), o = n == -INFINITY ? 0.f : n;
-            sum = sum * __builtin_amdgcn_exp2f((m - o) * kLog2e) +
-                  b.y * __builtin_amdgcn_exp2f((b.x - o) * kLog2e);
-            m = n;
+    __shared__ float2 s[256];
+    const int x = threadIdx.x % tok, y = threadIdx.x / tok, lanes = 256 / tok;
+    const int64_t t = (int64_t)blockIdx.x * tok + x;
+    float2 a = make_float2(-INFINITY, 0.f);
+    if (t < tokens) {
+        constexpr int kAhead = 4;
+        for (int32_t k = y; k < parts; k += kAhead * lanes) {
+            float2 b[kAhead];
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u)
+                b[u] = k + u * lanes < parts ? part[(int64_t)(k + u * lanes) * tpad + t]
+                                             : make_float2(-INFINITY, 0.f);
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) a = join(a, b[u]);
         }
-    s[y][x] = make_float2(m, sum);
-    __syncthreads();
+    }
+    s[threadIdx.x] = a;
+    for (int d = lanes / 2; d > 0; d >>= 1) {
+        __syncthreads();
+        if (y < d) s[threadIdx.x] = a = join(a, s[threadIdx.x + d * tok]);
+    }
     if (y != 0 || t >= tokens) return;
-    float top = s[0][x].x;
-    for (int k = 1; k < 16; ++k) top = fmaxf(top, s[k][x].x);
-    sum = 0.f;
-    for (int k = 0; k < 16; ++k)
-        if (s[k][x].x != -INFINITY || s[k][x].y != 0.f)
-            sum += s[k][x].y * __builtin_amdgcn_exp2f((s[k][x].x - top) * kLog2e);
     const bool ok = is_target(targets[t], vocab);
-    const float l = top + __builtin_amdgcn_logf(sum) * kLn2;
+    const float l = a.x + __builtin_amdgcn_logf(a.y) * kLn2;
     lse[t] = ok ? l : 0.f;
     loss[t] = ok ? l - target_z[t] : 0.f;
 }
@@ -383,7 +393,7 @@ __global__ __launch_bounds__(256) void pad_rows_kernel(const uint16_t* src, int6
                                                        int64_t rows, int64_t cols,
                                                        const int64_t* targets, int64_t vocab,
                                                        uint16_t* dst, int64_t prows,
-                                                       int64_t pcols, int vec)
+                                                       int64_t pcols)
 {
     const int64_t per = pcols / 8, n = prows * per;
     for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < n;
@@ -392,8 +402,8 @@ __global__ __launch_bounds__(256) void pad_rows_kernel(const uint16_t* src, int6
         uint4 x = make_uint4(0, 0, 0, 0);
         if (r < rows && c < cols && (!targets || is_target(targets[r], vocab))) {
             const uint16_t* s = src + r * ld + c;
-            if (vec && c + 8 <= cols) {
-                x = *(const uint4*)s;
+            if (c + 8 <= cols) {
+                x = load8(s);
             } else {
                 uint32_t w[4] = {0, 0, 0, 0};
 #pragma unroll
@@ -413,12 +423,14 @@ hipError_t pad_rows(const uint16_t* src, int64_t ld, int64_t rows, int64_t cols,
     const int64_t blocks = div_up(prows * (pcols / 8), 256);
     if (blocks == 0) return hipSuccess;
     pad_rows_kernel<<<dim3((unsigned)(blocks < 4096 ? blocks : 4096)), dim3(256), 0, stream>>>(
-        src, ld, rows, cols, targets, vocab, dst, prows, pcols, rows_aligned(src, ld, 2, 16));
+        src, ld, rows, cols, targets, vocab, dst, prows, pcols);
     return hipGetLastError();
 }
 
 // ---- backward: G of a piece ---------------------------------------------------
 
+// kTerms: BF16 terms that G is kept in.
+template <int kTerms>
 struct GradEpi {
     struct Args {
         const int64_t* targets;
@@ -428,60 +440,81 @@ struct GradEpi {
         float* rest;           // [tpad]: what rounding took from the target's entry
         int64_t gld, term;     // row stride; elements between terms
         int64_t tpad, v0, vocab;
-        int32_t tokens, terms;
+        int32_t tokens;
         float scale;
     };
-
+    struct Rows {
+        static constexpr bool kMirror = false, kAhead = true;
+        struct Regs {
+            float lse, w;
+            int64_t target;    // -1: padding
+        };
+        const Args& e;
+        int64_t ni;
+        __device__ __forceinline__ void columns(int64_t) const {}
+        __device__ __forceinline__ void load(Regs& r, int64_t t, int64_t) const
+        {
+            r.lse = r.w = 0.f;
+            r.target = -1;
+            if (t < e.tokens) {
+                r.target = e.targets[t];
+                r.lse = e.lse[t];
+                r.w = e.grad_loss[t];
+            }
+        }
+        __device__ __forceinline__ void put(const Regs& r, int64_t t, int64_t ii,
+                                            float (&x)[8]) const
+        {
+            if (t >= e.tpad || ii >= e.gld) return;
+            const bool ok = is_target(r.target, e.vocab);
+            const float w = r.w * e.scale;
+            if constexpr (kTerms == 1) {
+                const float c = e.scale * kLog2e, o = r.lse * kLog2e;
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    x[k] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[k], c, -o));
+            } else {
+                // the difference before the change of base: exact to the
+                // rounding of the product
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    x[k] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[k], e.scale, -r.lse) * kLog2e);
+            }
+            const int64_t hot = r.target - e.v0 - ii;
+            if (ok && hot >= 0 && hot < 8) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (hot == k) {
+                        x[k] -= 1.f;
+                        e.rest[t] = x[k] * w - from_bf16(to_bf16(x[k] * w));
+                    }
+            }
+            if (ii + 8 > ni) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (ii + k >= ni) x[k] = 0.f;
+            }
+            uint16_t* dst = e.g + t * e.gld + ii;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) x[k] *= w;
+#pragma unroll
+            for (int n = 0; n < kTerms; ++n) {
+                const uint4 h = bf16x8(x);
+                *(uint4*)(dst + n * e.term) = ok ? h : make_uint4(0, 0, 0, 0);
+                if (n + 1 < kTerms) {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) x[k] -= from_bf16(at8(h, k));
+                }
+            }
+        }
+    };
     template <class S>
     static __device__ __forceinline__ void run(const Args& e, const pr::ProductArgs& p,
                                                const pr::TileAt& at, const pr::LanePos<S>& pos,
                                                f32x4 (&acc)[S::FI][S::FJ])
     {
-#pragma unroll
-        for (int j = 0; j < S::FJ; ++j) {
-            const int64_t t = pos.j + 16 * j;
-            if (t >= e.tpad) continue;
-            int64_t target = -1;
-            float lse = 0.f, w = 0.f;
-            bool ok = false;
-            if (t < e.tokens) {
-                target = e.targets[t];
-                ok = is_target(target, e.vocab);
-                lse = e.lse[t];
-                w = e.grad_loss[t] * e.scale;
-            }
-            const int64_t hot = target - e.v0 - pos.i;
-#pragma unroll
-            for (int i = 0; i < S::FI; ++i) {
-                if (pos.i + 16 * i >= e.gld) continue;
-                f32x4 g;
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    // the difference is taken before the change of base: exact
-                    // to the rounding of the product
-                    float x = __builtin_amdgcn_exp2f(
-                        __builtin_fmaf(acc[i][j][r], e.scale, -lse) * kLog2e);
-                    if (hot == 16 * i + r) x -= 1.f;
-                    g[r] = ok && pos.i + 16 * i + r < p.ni ? x * w : 0.f;
-                }
-                const f32x4 whole = g;
-                uint16_t* dst = e.g + t * e.gld + pos.i + 16 * i;
-                for (int k = 0; k < e.terms; ++k) {
-                    uint16_t h[4];
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        h[r] = to_bf16(g[r]);
-                        g[r] -= from_bf16(h[r]);
-                    }
-                    *(uint2*)(dst + k * e.term) = make_uint2(h[0] | (uint32_t)h[1] << 16,
-                                                             h[2] | (uint32_t)h[3] << 16);
-                }
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    if (ok && hot == 16 * i + r)
-                        e.rest[t] = whole[r] - from_bf16(to_bf16(whole[r]));
-            }
-        }
+        Rows f{e, p.ni};
+        pr::for_rows<S>(pos, acc, f);
     }
 };
 
@@ -494,75 +527,111 @@ struct SumEpi {
         int64_t ld, part;      // elements between the splits' parts
         int32_t add;
     };
-    template <class S>
-    static __device__ __forceinline__ void run(const Args& e, const pr::ProductArgs& p,
-                                               const pr::TileAt& at, const pr::LanePos<S>& pos,
-                                               f32x4 (&acc)[S::FI][S::FJ])
-    {
-        float* out = e.out + at.split * e.part;
-#pragma unroll
-        for (int j = 0; j < S::FJ; ++j) {
-            const int64_t jj = pos.j + 16 * j;
-            if (jj >= p.nj) continue;
-#pragma unroll
-            for (int i = 0; i < S::FI; ++i) {
-                const int64_t ii = pos.i + 16 * i;
-                if (ii >= p.ni) continue;
-                f32x4* q = (f32x4*)(out + jj * e.ld + ii);
-                *q = e.add ? *q + acc[i][j] : acc[i][j];
-            }
+    struct Rows {
+        static constexpr bool kMirror = false, kAhead = true;
+        struct Regs {
+            f32x4 x[2];
+        };
+        const Args& e;
+        float* out;
+        int64_t ni, nj;
+        __device__ __forceinline__ void columns(int64_t) const {}
+        __device__ __forceinline__ void load(Regs& r, int64_t jj, int64_t ii) const
+        {
+            if (!e.add || jj >= nj || ii >= ni) return;
+            const f32x4* q = (const f32x4*)(out + jj * e.ld + ii);
+            r.x[0] = q[0];
+            r.x[1] = q[1];
         }
-    }
-};
-
-// The user's weight gradient: any stride and alignment.
-struct WeightGradEpi {
-    struct Args {
-        void* out;
-        int64_t ld;
-        int32_t f32, add, vec;  // vec: rows 16-byte (F32) or 8-byte (BF16) aligned
+        __device__ __forceinline__ void put(const Regs& r, int64_t jj, int64_t ii,
+                                            float (&x)[8]) const
+        {
+            if (jj >= nj || ii >= ni) return;
+            f32x4* q = (f32x4*)(out + jj * e.ld + ii);
+            f32x4 a = f32x4{x[0], x[1], x[2], x[3]}, b = f32x4{x[4], x[5], x[6], x[7]};
+            if (e.add) {
+                a += r.x[0];
+                b += r.x[1];
+            }
+            q[0] = a;
+            q[1] = b;
+        }
     };
     template <class S>
     static __device__ __forceinline__ void run(const Args& e, const pr::ProductArgs& p,
                                                const pr::TileAt& at, const pr::LanePos<S>& pos,
                                                f32x4 (&acc)[S::FI][S::FJ])
     {
-#pragma unroll
-        for (int j = 0; j < S::FJ; ++j) {
-            const int64_t jj = pos.j + 16 * j;
-            if (jj >= p.nj) continue;
-#pragma unroll
-            for (int i = 0; i < S::FI; ++i) {
-                const int64_t ii = pos.i + 16 * i;
-                if (ii >= p.ni) continue;
-                const bool vec = e.vec && ii + 4 <= p.ni;
-                f32x4 x = acc[i][j];
-                if (e.f32) {
-                    float* q = (float*)e.out + jj * e.ld + ii;
-                    if (vec) {
-                        if (e.add) x += *(f32x4*)q;
-                        *(f32x4*)q = x;
-                    } else {
-#pragma unroll
-                        for (int r = 0; r < 4; ++r)
-                            if (ii + r < p.ni) q[r] = e.add ? q[r] + x[r] : x[r];
+        Rows f{e, e.out + at.split * e.part, p.ni, p.nj};
+        pr::for_rows<S>(pos, acc, f);
+    }
+};
+
+// The user's weight gradient: any stride and alignment.
+template <bool kF32>
+struct WeightGradEpi {
+    struct Args {
+        void* out;
+        int64_t ld;
+        int32_t add;           // (F32)
+    };
+    struct Rows {
+        static constexpr bool kMirror = false, kAhead = kF32;
+        struct Regs {
+            f32x4_any x[kF32 ? 2 : 1];
+        };
+        const Args& e;
+        int64_t ni, nj;
+        __device__ __forceinline__ void columns(int64_t) const {}
+        __device__ __forceinline__ void load(Regs& r, int64_t jj, int64_t ii) const
+        {
+            if constexpr (kF32) {
+                if (!e.add || jj >= nj || ii + 8 > ni) return;
+                const f32x4_any* q = (const f32x4_any*)((const float*)e.out + jj * e.ld + ii);
+                r.x[0] = q[0];
+                r.x[1] = q[1];
+            }
+        }
+        __device__ __forceinline__ void put(const Regs& r, int64_t jj, int64_t ii,
+                                            float (&x)[8]) const
+        {
+            if (jj >= nj || ii >= ni) return;
+            if constexpr (kF32) {
+                float* q = (float*)e.out + jj * e.ld + ii;
+                if (ii + 8 <= ni) {
+                    f32x4_any a = f32x4_any{x[0], x[1], x[2], x[3]};
+                    f32x4_any b = f32x4_any{x[4], x[5], x[6], x[7]};
+                    if (e.add) {
+                        a += r.x[0];
+                        b += r.x[1];
                     }
+                    ((f32x4_any*)q)[0] = a;
+                    ((f32x4_any*)q)[1] = b;
                 } else {
-                    uint16_t* q = (uint16_t*)e.out + jj * e.ld + ii;
-                    uint16_t h[4];
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) h[r] = to_bf16(x[r]);
-                    if (vec) {
-                        *(uint2*)q = make_uint2(h[0] | (uint32_t)h[1] << 16,
-                                                h[2] | (uint32_t)h[3] << 16);
-                    } else {
+                    for (int k = 0; k < 8; ++k)
+                        if (ii + k < ni) q[k] = e.add ? q[k] + x[k] : x[k];
+                }
+            } else {
+                uint16_t* q = (uint16_t*)e.out + jj * e.ld + ii;
+                const uint4 h = bf16x8(x);
+                if (ii + 8 <= ni) {
+                    store8(q, h);
+                } else {
 #pragma unroll
-                        for (int r = 0; r < 4; ++r)
-                            if (ii + r < p.ni) q[r] = h[r];
-                    }
+                    for (int k = 0; k < 8; ++k)
+                        if (ii + k < ni) q[k] = at8(h, k);
                 }
             }
         }
+    };
+    template <class S>
+    static __device__ __forceinline__ void run(const Args& e, const pr::ProductArgs& p,
+                                               const pr::TileAt& at, const pr::LanePos<S>& pos,
+                                               f32x4 (&acc)[S::FI][S::FJ])
+    {
+        Rows f{e, p.ni, p.nj};
+        pr::for_rows<S>(pos, acc, f);
     }
 };
 
@@ -577,32 +646,40 @@ __global__ __launch_bounds__(256) void hidden_grad_kernel(const float* part, int
                                                           const int64_t* targets, int64_t vocab,
                                                           const uint16_t* weight,
                                                           int64_t weight_ld, uint16_t* out,
-                                                          int64_t ld, int vec)
+                                                          int64_t ld)
 {
-    const int64_t per = (cols + 3) / 4, n = rows * per;
+    const int64_t per = (cols + 7) / 8, n = rows * per;
     for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < n;
          q += (int64_t)gridDim.x * 256) {
-        const int64_t r = q / per, c = (q - r * per) * 4;
-        f32x4 x = *(const f32x4*)(part + r * pld + c);
-        for (int32_t s = 1; s < splits; ++s)
-            x += *(const f32x4*)(part + s * stride + r * pld + c);
+        const int64_t r = q / per, c = (q - r * per) * 8;
         const int64_t target = targets[r];
-        if (is_target(target, vocab)) {
-            const uint16_t* w = weight + target * weight_ld + c;
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-                if (c + k < cols) x[k] += rest[r] * from_bf16(w[k]);
-        }
-        uint16_t h[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) h[k] = to_bf16(x[k]);
         uint16_t* o = out + r * ld + c;
-        if (vec && c + 4 <= cols) {
-            *(uint2*)o = make_uint2(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16);
+        float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (is_target(target, vocab)) {
+            const float* p = part + r * pld + c;
+            const uint16_t* w = weight + target * weight_ld + c;
+            const float f = rest[r];
+            uint4 wv = make_uint4(0, 0, 0, 0);
+            if (c + 8 <= cols) wv = load8(w);
+            f32x4 a = f32x4(0.f), b = f32x4(0.f);
+            for (int32_t s = 0; s < splits; ++s) {
+                a += *(const f32x4*)(p + s * stride);
+                b += *(const f32x4*)(p + s * stride + 4);
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const float wk = c + 8 <= cols ? from_bf16(at8(wv, k))
+                                 : c + k < cols ? from_bf16(w[k]) : 0.f;
+                x[k] = (k < 4 ? a[k & 3] : b[k & 3]) + f * wk;
+            }
+        }
+        const uint4 h = bf16x8(x);
+        if (c + 8 <= cols) {
+            store8(o, h);
         } else {
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-                if (c + k < cols) o[k] = h[k];
+            for (int k = 0; k < 8; ++k)
+                if (c + k < cols) o[k] = at8(h, k);
         }
     }
 }
@@ -638,6 +715,29 @@ ShapeKind shape_for(int64_t ni, int64_t nj, int cus)
 }
 
 constexpr int64_t kPieceBytes = (int64_t)256 << 20;   // of G
+
+// Tiles of grad_hidden and how many blocks share a tile's vocabulary rows (few
+// tiles would leave CUs idle): the shape whose rounds take least, as in
+// pr::tiles_for, with at least 16 steps for each block.
+void hidden_shape(Sizes* s, int cus)
+{
+    const int64_t T = s->T > 0 ? s->T : 1, most = div_up(s->piece, 64 * 16);
+    auto split = [&](int64_t tiles, int64_t slots) {
+        const int64_t x = slots / tiles;
+        return x < 1 ? 1 : x > most ? most : x > 64 ? 64 : x;
+    };
+    if (T <= 64) {
+        s->hid = T <= 32 ? kThin32 : kThin64;
+        s->split = (int32_t)split(div_up(s->d, 256), cus);
+        return;
+    }
+    const int64_t tl = div_up(s->d, 256) * div_up(T, 256), sl = split(tl, cus);
+    const int64_t tm = div_up(s->d, 128) * div_up(T, 128), sm = split(tm, 2 * cus);
+    const double large = (double)div_up(tl * sl, cus) / sl;
+    const double medium = tm * sm <= cus ? 0.4 / sm : (double)div_up(tm * sm, 2 * cus) / sm * 0.62;
+    s->hid = large <= medium ? kLarge : tm * sm <= cus ? kDeep : kMedium;
+    s->split = (int32_t)(large <= medium ? sl : sm);
+}
 
 bool sizes_of(const dte_linear_ce* c, bool backward, int32_t grad_type, Sizes* s)
 {
@@ -679,19 +779,13 @@ bool sizes_of(const dte_linear_ce* c, bool backward, int32_t grad_type, Sizes* s
         if (most < 4096) most = 4096;
         if (cols > most) cols = most;
     }
+    // whole rounds of 256 x 256 tiles, where that takes no more than a piece
+    const int64_t unit = 256 * (cus / std::gcd((int64_t)cus, div_up(s->T ? s->T : 1, 256)));
+    if (cols > unit) cols = cols / unit * unit;
     s->piece = cols < s->V ? cols : s->V;
     s->gld = round_up(s->piece, 64);
-    s->hid = shape_for(s->d, s->T, cus);
     s->wgt = shape_for(s->d, s->piece > 64 ? s->piece : 65, cus);
-    // few tiles of grad_hidden: share each tile's vocabulary rows among blocks
-    const int64_t ti = tile_i(s->hid);
-    const int64_t tj = s->hid == kLarge ? 256 : tile_i(s->hid) == 128 ? 128 : s->hid == kThin64 ? 64 : 32;
-    const int64_t tiles = div_up(s->d, ti) * div_up(s->T > 0 ? s->T : 1, tj);
-    const int64_t slots = s->hid == kLarge ? cus : 2 * cus;
-    int64_t split = slots / tiles;
-    const int64_t most = div_up(s->piece, 64 * 4);   // at least four steps each
-    if (split > most) split = most;
-    s->split = (int32_t)(split < 1 ? 1 : split > 64 ? 64 : split);
+    hidden_shape(s, cus);
     return true;
 }
 
@@ -802,8 +896,9 @@ dte_status forward(const dte_linear_ce* c, const Sizes& s, const Buffers& b, flo
         DTE_TRY((product<pr::kK, pr::kK, StatsEpi>(s.logits, p, e, st)));
         part0 += (int32_t)div_up(n, tile_i(s.logits));
     }
-    join_stats_kernel<<<dim3((unsigned)div_up(s.T, 16)), dim3(256), 0, st>>>(
-        b.part, s.tpad, part0, b.target_z, c->targets, s.V, (int32_t)s.T, loss, lse);
+    const int32_t tok = s.T <= 64 ? 4 : 16;
+    join_stats_kernel<<<dim3((unsigned)div_up(s.T, tok)), dim3(256), 0, st>>>(
+        b.part, s.tpad, part0, tok, b.target_z, c->targets, s.V, (int32_t)s.T, loss, lse);
     DTE_TRY(hipGetLastError());
     return DTE_OK;
 }
@@ -820,10 +915,15 @@ dte_status backward(const dte_linear_ce* c, const Sizes& s, const Buffers& b, co
         DTE_TRY(weight_rows(c, s, b, v0, n, st, &w));
         {
             const pr::ProductArgs p = logits_product(s, b, w, n);
-            const GradEpi::Args e{c->targets, lse,  grad_loss, b.g, b.rest,       s.gld,
-                                  s.tpad * s.gld, s.tpad, v0, s.V, (int32_t)s.T, s.terms,
-                                  c->scale};
-            DTE_TRY((product<pr::kK, pr::kK, GradEpi>(s.logits, p, e, st)));
+            auto grad = [&](auto terms) {
+                typedef GradEpi<decltype(terms)::value> Epi;
+                const typename Epi::Args e{c->targets, lse,    grad_loss, b.g,
+                                           b.rest,     s.gld,  s.tpad * s.gld,
+                                           s.tpad,     v0,     s.V, (int32_t)s.T, c->scale};
+                return product<pr::kK, pr::kK, Epi>(s.logits, p, e, st);
+            };
+            DTE_TRY(s.terms == 1 ? grad(std::integral_constant<int, 1>())
+                                 : grad(std::integral_constant<int, 3>()));
         }
         if (gh) {
             pr::ProductArgs p{};
@@ -848,17 +948,20 @@ dte_status backward(const dte_linear_ce* c, const Sizes& s, const Buffers& b, co
             p.split = 1;
             p.batch = 1;
             void* out = (char*)gw + v0 * gw_ld * size;
-            const WeightGradEpi::Args e{out, gw_ld, type == DTE_TYPE_F32, accumulate != 0,
-                                        rows_aligned(gw, gw_ld, size, 4 * size)};
-            DTE_TRY((product<pr::kR, pr::kR, WeightGradEpi>(s.wgt, p, e, st)));
+            if (type == DTE_TYPE_F32) {
+                const WeightGradEpi<true>::Args e{out, gw_ld, accumulate != 0};
+                DTE_TRY((product<pr::kR, pr::kR, WeightGradEpi<true>>(s.wgt, p, e, st)));
+            } else {
+                const WeightGradEpi<false>::Args e{out, gw_ld, 0};
+                DTE_TRY((product<pr::kR, pr::kR, WeightGradEpi<false>>(s.wgt, p, e, st)));
+            }
         }
     }
     if (gh) {
-        const int64_t blocks = div_up(s.T * div_up(s.d, 4), 256);
+        const int64_t blocks = div_up(s.T * div_up(s.d, 8), 256);
         hidden_grad_kernel<<<dim3((unsigned)(blocks < 8192 ? blocks : 8192)), dim3(256), 0, st>>>(
             b.hsum, s.tpad * s.dpad, s.split, s.dpad, s.T, s.d, b.rest, c->targets, s.V,
-            c->weight, c->weight_ld, gh, gh_ld,
-            rows_aligned(gh, gh_ld, 2, 8));
+            c->weight, c->weight_ld, gh, gh_ld);
         DTE_TRY(hipGetLastError());
     }
     return DTE_OK;

@@ -59,6 +59,27 @@ __device__ __forceinline__ uint32_t pack(uint16_t lo, uint16_t hi)
 {
     return lo | (uint32_t)hi << 16;
 }
+// Vectors at any element's address (the hardware takes them; aligned ones are
+// a little faster by themselves).
+typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint16_t u16x4_any __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint16_t u16x8_any __attribute__((ext_vector_type(8), aligned(2)));
+
+__device__ __forceinline__ uint4 load8(const uint16_t* p)
+{
+    return __builtin_bit_cast(uint4, *(const u16x8_any*)p);
+}
+__device__ __forceinline__ void store8(uint16_t* p, uint4 x)
+{
+    *(u16x8_any*)p = __builtin_bit_cast(u16x8_any, x);
+}
+// Value k of eight 16-bit ones.
+__device__ __forceinline__ uint16_t at8(const uint4& w, int k)
+{
+    const uint32_t u = k < 2 ? w.x : k < 4 ? w.y : k < 6 ? w.z : w.w;
+    return (uint16_t)(k & 1 ? u >> 16 : u);
+}
+
 // Eight values as BF16.
 __device__ __forceinline__ uint4 bf16x8(const float (&x)[8])
 {
