@@ -28,26 +28,27 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 // ---- forward ------------------------------------------------------------------
 
-// kCols columns of a thread: contiguous (16 bytes) or, where rows do not
-// begin at 16-byte addresses, strided by the wave.
+// 16 bytes of a row, at any element's address, and the values in them.
 template <typename T>
 struct Row;
 template <>
 struct Row<float> {
     static constexpr int kCols = 4;
+    typedef f32x4_any vec;
     static __device__ __forceinline__ float value(float x) { return x; }
     static __device__ __forceinline__ float make(float x) { return x; }
 };
 template <>
 struct Row<uint16_t> {
     static constexpr int kCols = 8;
+    typedef u16x8_any vec;
     static __device__ __forceinline__ float value(uint16_t x) { return from_bf16(x); }
     static __device__ __forceinline__ uint16_t make(float x) { return to_bf16(x); }
 };
 
 constexpr int kSegVecs = 256;      // vectors of a row that one wave takes: 4 per lane
 
-template <typename T, bool kAligned>
+template <typename T>
 __global__ __launch_bounds__(256) void embedding_rows_kernel(const T* table, int64_t vocab,
                                                              int64_t hidden, int64_t table_ld,
                                                              const int64_t* ids, int64_t n,
@@ -55,6 +56,7 @@ __global__ __launch_bounds__(256) void embedding_rows_kernel(const T* table, int
                                                              int32_t segs)
 {
     constexpr int kCols = Row<T>::kCols;
+    typedef typename Row<T>::vec vec;
     const int lane = threadIdx.x & 63;
     const int64_t unit = (int64_t)blockIdx.x * 4 +
                          __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -65,32 +67,25 @@ __global__ __launch_bounds__(256) void embedding_rows_kernel(const T* table, int
     const bool ok = id >= 0 && id < vocab;
     const T* src = table + (ok ? id : 0) * table_ld;
     T* dst = out + r * out_ld;
-    if constexpr (kAligned) {
-        typedef T vec __attribute__((ext_vector_type(kCols)));
-        const int64_t c0 = (int64_t)seg * kSegVecs * kCols + lane * kCols;
-        vec x[4];
+    const int64_t c0 = (int64_t)seg * kSegVecs * kCols + lane * kCols;
+    vec x[4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const int64_t c = c0 + k * 64 * kCols;
-            x[k] = ok && c < hidden ? *(const vec*)(src + c) : vec(0);
-        }
+    for (int k = 0; k < 4; ++k) {
+        const int64_t c = c0 + k * 64 * kCols;
+        x[k] = ok && c + kCols <= hidden ? *(const vec*)(src + c) : vec(0);
+    }
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const int64_t c = c0 + k * 64 * kCols;
-            if (c >= hidden) break;
+    for (int k = 0; k < 4; ++k) {
+        const int64_t c = c0 + k * 64 * kCols;
+        if (c + kCols <= hidden) {
             vec y;
 #pragma unroll
             for (int i = 0; i < kCols; ++i)
                 y[i] = ok ? Row<T>::make(scale * Row<T>::value(x[k][i])) : T(0);
             *(vec*)(dst + c) = y;
-        }
-    } else {
-        const int64_t c0 = (int64_t)seg * kSegVecs * kCols;
-#pragma unroll 4
-        for (int k = 0; k < 4 * kCols; ++k) {
-            const int64_t c = c0 + k * 64 + lane;
-            if (c >= hidden) break;
-            dst[c] = ok ? Row<T>::make(scale * Row<T>::value(src[c])) : T(0);
+        } else {
+            for (int64_t i = c; i < hidden; ++i)
+                dst[i] = ok ? Row<T>::make(scale * Row<T>::value(src[i])) : T(0);
         }
     }
 }
@@ -103,17 +98,8 @@ hipError_t launch_rows(const void* table, int64_t vocab, int64_t hidden, int64_t
     const int64_t segs = div_up(hidden, (int64_t)kSegVecs * Row<T>::kCols);
     const int64_t blocks = div_up(n * segs, 4);
     if (blocks > 0x7fffffff) return hipErrorInvalidValue;
-    const bool aligned = rows_aligned(table, table_ld, sizeof(T), 16) &&
-                         rows_aligned(out, out_ld, sizeof(T), 16) &&
-                         hidden % Row<T>::kCols == 0;
-    if (aligned)
-        embedding_rows_kernel<T, true><<<dim3((unsigned)blocks), dim3(256), 0, st>>>(
-            (const T*)table, vocab, hidden, table_ld, ids, n, scale, (T*)out, out_ld,
-            (int32_t)segs);
-    else
-        embedding_rows_kernel<T, false><<<dim3((unsigned)blocks), dim3(256), 0, st>>>(
-            (const T*)table, vocab, hidden, table_ld, ids, n, scale, (T*)out, out_ld,
-            (int32_t)segs);
+    embedding_rows_kernel<T><<<dim3((unsigned)blocks), dim3(256), 0, st>>>(
+        (const T*)table, vocab, hidden, table_ld, ids, n, scale, (T*)out, out_ld, (int32_t)segs);
     return hipGetLastError();
 }
 
@@ -199,10 +185,15 @@ __global__ __launch_bounds__(kSortThreads) void sort_pass_kernel(SortPlan p, int
     // totals of each digit, and its counts in the blocks before this one
     int32_t total = 0, before = 0;
     if (tid < bins)
-        for (int32_t b = 0; b < p.blocks; ++b) {
-            const int32_t c = hist[b * bins + tid];
-            total += c;
-            before += b < (int32_t)blockIdx.x ? c : 0;
+        for (int32_t b = 0; b < p.blocks; b += 8) {
+            int32_t c[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) c[u] = b + u < p.blocks ? hist[(b + u) * bins + tid] : 0;
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                total += c[u];
+                before += b + u < (int32_t)blockIdx.x ? c[u] : 0;
+            }
         }
     int32_t scan = total;                               // inclusive over the digits
 #pragma unroll
@@ -278,112 +269,143 @@ struct SumArgs {
     int32_t n, vocab, chunk, chunks, zero_blocks, out_f32, accumulate;
 };
 
-template <int kCols, bool kAligned>
+// kCols consecutive columns of a thread; `whole`: all of them exist.
+template <int kCols>
 struct Columns {
-    int64_t first, stride;
-    int64_t hidden;
-    __device__ __forceinline__ Columns(int64_t h)
+    int64_t first;
+    int count;
+    bool whole;
+    __device__ __forceinline__ Columns(int64_t hidden)
     {
-        const int64_t slab = (int64_t)blockIdx.y * blockDim.x * kCols;
-        first = kAligned ? slab + threadIdx.x * kCols : slab + threadIdx.x;
-        stride = kAligned ? 1 : blockDim.x;
-        hidden = h;
+        first = ((int64_t)blockIdx.y * blockDim.x + threadIdx.x) * kCols;
+        const int64_t left = hidden - first;
+        count = left < 0 ? 0 : left < kCols ? (int)left : kCols;
+        whole = count == kCols;
     }
-    __device__ __forceinline__ int64_t col(int k) const { return first + k * stride; }
-    __device__ __forceinline__ bool has(int k) const { return col(k) < hidden; }
 };
 
-template <typename T, bool kAligned>
-__device__ __forceinline__ void load_row(const T* row, const Columns<Row<T>::kCols, kAligned>& c,
+template <typename T>
+__device__ __forceinline__ void load_row(const T* row, const Columns<Row<T>::kCols>& c,
                                          float (&x)[Row<T>::kCols])
 {
     constexpr int kCols = Row<T>::kCols;
-    if constexpr (kAligned) {
-        typedef T vec __attribute__((ext_vector_type(kCols)));
-        const vec y = c.has(0) ? *(const vec*)(row + c.first) : vec(0);
+    if (c.whole) {
+        const typename Row<T>::vec y = *(const typename Row<T>::vec*)(row + c.first);
 #pragma unroll
         for (int k = 0; k < kCols; ++k) x[k] = Row<T>::value(y[k]);
     } else {
 #pragma unroll
-        for (int k = 0; k < kCols; ++k) x[k] = c.has(k) ? Row<T>::value(row[c.col(k)]) : 0.f;
+        for (int k = 0; k < kCols; ++k) x[k] = k < c.count ? Row<T>::value(row[c.first + k]) : 0.f;
     }
 }
 
-// A finished row of the table's gradient.
-template <int kCols, bool kAligned>
-__device__ __forceinline__ void store_row(const SumArgs& a, const Columns<kCols, kAligned>& c,
-                                          int64_t token, const float (&x)[kCols])
+// What a finished row is added to.
+template <int kCols>
+__device__ __forceinline__ void load_old(const SumArgs& a, const Columns<kCols>& c, int64_t token,
+                                         float (&x)[kCols])
+{
+    const float* o = (const float*)a.out + token * a.out_ld + c.first;
+    if (c.whole) {
+#pragma unroll
+        for (int k = 0; k < kCols; k += 4) {
+            const f32x4_any y = *(const f32x4_any*)(o + k);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) x[k + r] = y[r];
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < kCols; ++k) x[k] = k < c.count ? o[k] : 0.f;
+    }
+}
+
+// A finished row of the table's gradient; kAdd: added to old.
+template <int kCols, bool kAdd>
+__device__ __forceinline__ void store_row(const SumArgs& a, const Columns<kCols>& c,
+                                          int64_t token, const float (&x)[kCols],
+                                          const float (&old)[kCols])
 {
     if (a.out_f32) {
-        float* o = (float*)a.out + token * a.out_ld;
-        if constexpr (kAligned) {
-            if (!c.has(0)) return;
+        float* o = (float*)a.out + token * a.out_ld + c.first;
+        if (c.whole) {
 #pragma unroll
             for (int k = 0; k < kCols; k += 4) {
-                f32x4 y = f32x4{a.scale * x[k], a.scale * x[k + 1], a.scale * x[k + 2],
-                                a.scale * x[k + 3]};
-                f32x4* q = (f32x4*)(o + c.first + k);
-                if (a.accumulate) y += *q;
-                *q = y;
+                f32x4_any y = f32x4_any{a.scale * x[k], a.scale * x[k + 1], a.scale * x[k + 2],
+                                        a.scale * x[k + 3]};
+                if constexpr (kAdd) y += f32x4_any{old[k], old[k + 1], old[k + 2], old[k + 3]};
+                *(f32x4_any*)(o + k) = y;
             }
         } else {
 #pragma unroll
             for (int k = 0; k < kCols; ++k)
-                if (c.has(k)) {
-                    float* q = o + c.col(k);
-                    *q = a.accumulate ? *q + a.scale * x[k] : a.scale * x[k];
-                }
+                if (k < c.count) o[k] = kAdd ? old[k] + a.scale * x[k] : a.scale * x[k];
         }
     } else {
-        uint16_t* o = (uint16_t*)a.out + token * a.out_ld;
-        if constexpr (kAligned) {
-            if (!c.has(0)) return;
+        uint16_t* o = (uint16_t*)a.out + token * a.out_ld + c.first;
+        if (c.whole) {
 #pragma unroll
-            for (int k = 0; k < kCols; k += 4) {
-                uint16_t h[4];
-#pragma unroll
-                for (int r = 0; r < 4; ++r) h[r] = to_bf16(a.scale * x[k + r]);
-                *(uint2*)(o + c.first + k) = make_uint2(h[0] | (uint32_t)h[1] << 16,
-                                                        h[2] | (uint32_t)h[3] << 16);
-            }
+            for (int k = 0; k < kCols; k += 4)
+                *(u16x4_any*)(o + k) = u16x4_any{to_bf16(a.scale * x[k]),
+                                                 to_bf16(a.scale * x[k + 1]),
+                                                 to_bf16(a.scale * x[k + 2]),
+                                                 to_bf16(a.scale * x[k + 3])};
         } else {
 #pragma unroll
             for (int k = 0; k < kCols; ++k)
-                if (c.has(k)) o[c.col(k)] = to_bf16(a.scale * x[k]);
+                if (k < c.count) o[k] = to_bf16(a.scale * x[k]);
         }
     }
 }
 
-template <int kCols, bool kAligned>
-__device__ __forceinline__ void store_part(const SumArgs& a, const Columns<kCols, kAligned>& c,
-                                           int64_t row, const float (&x)[kCols])
+// Zeros for the rows of tokens that do not occur: a wave looks at 64 flags at
+// once and writes the rows 1 KB at a time.  (Stores past the caches are no
+// faster: 151936 x 4096 in binary32, of which 16384 rows occur at most, 525 us
+// either way, 5.0 TB/s.)
+__device__ __forceinline__ void zero_rows(const SumArgs& a, int64_t wave, int64_t waves)
 {
-    float* o = a.part + row * a.pld;
-    if constexpr (kAligned) {
-        if (!c.has(0)) return;
-#pragma unroll
-        for (int k = 0; k < kCols; k += 4)
-            *(f32x4*)(o + c.first + k) = f32x4{x[k], x[k + 1], x[k + 2], x[k + 3]};
-    } else {
-#pragma unroll
-        for (int k = 0; k < kCols; ++k)
-            if (c.has(k)) o[c.col(k)] = x[k];
+    const int lane = threadIdx.x & 63;
+    const int64_t size = a.out_f32 ? 4 : 2, bytes = a.hidden * size;
+    for (int64_t v0 = wave * 64; v0 < a.vocab; v0 += waves * 64) {
+        uint64_t todo = __ballot(v0 + lane < a.vocab && !a.flags[v0 + lane]);
+        while (todo) {
+            const int64_t v = v0 + __builtin_ctzll(todo);
+            todo &= todo - 1;
+            char* row = (char*)a.out + v * a.out_ld * size;
+            const u16x8_any zero = u16x8_any(0);
+            int64_t c = lane * 16;
+            for (; c + 16 <= bytes; c += 1024) *(u16x8_any*)(row + c) = zero;
+            for (; c < bytes; c += size) {     // the lane that the row ends in
+                if (size == 4)
+                    *(float*)(row + c) = 0.f;
+                else
+                    *(uint16_t*)(row + c) = 0;
+            }
+        }
     }
 }
 
-template <typename T, bool kAligned>
+// Partial rows are padded to whole vectors.
+template <int kCols>
+__device__ __forceinline__ void store_part(const SumArgs& a, const Columns<kCols>& c, int64_t row,
+                                           const float (&x)[kCols])
+{
+    if (c.count == 0) return;
+    float* o = a.part + row * a.pld + c.first;
+#pragma unroll
+    for (int k = 0; k < kCols; k += 4) *(f32x4*)(o + k) = f32x4{x[k], x[k + 1], x[k + 2], x[k + 3]};
+}
+
+// kAdd: accumulate (the rows to add to are fetched with the gradient's).
+template <typename T, bool kAdd>
 __global__ __launch_bounds__(256) void embedding_sum_kernel(SumArgs a)
 {
     constexpr int kCols = Row<T>::kCols;
     __shared__ int2 s_item[kMaxChunk + 2];     // the entry before, the chunk, the entry after
-    const Columns<kCols, kAligned> c(a.hidden);
-    float zero[kCols];
-#pragma unroll
-    for (int k = 0; k < kCols; ++k) zero[k] = 0.f;
+    const Columns<kCols> c(a.hidden);
     if (blockIdx.x >= (unsigned)a.chunks) {
-        // rows of tokens that do not occur
-        for (int64_t v = (int64_t)blockIdx.x - a.chunks; v < a.vocab; v += a.zero_blocks)
-            if (!a.flags[v]) store_row<kCols, kAligned>(a, c, v, zero);
+        const int per = blockDim.x / 64;
+        const int64_t block = (int64_t)(blockIdx.x - a.chunks) * gridDim.y + blockIdx.y;
+        zero_rows(a, block * per + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6),
+                  (int64_t)a.zero_blocks * gridDim.y * per);
         return;
     }
     const int32_t begin = blockIdx.x * a.chunk;
@@ -398,13 +420,18 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(SumArgs a)
 #pragma unroll
     for (int k = 0; k < kCols; ++k) acc[k] = 0.f;
     bool entered = s_item[0].x == s_item[1].x;
-    constexpr int kAhead = 4;
+    constexpr int kAhead = kAdd ? 32 / kCols : 8;
     for (int32_t e0 = 0; e0 < count; e0 += kAhead) {
-        float x[kAhead][kCols];
+        float x[kAhead][kCols], old[kAdd ? kAhead : 1][kCols];
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
             const int2 it = s_item[1 + (e0 + u < count ? e0 + u : e0)];
-            if (it.x < a.vocab) load_row<T, kAligned>(grad + it.y * a.grad_ld, c, x[u]);
+            if (it.x >= a.vocab) continue;
+            load_row<T>(grad + it.y * a.grad_ld, c, x[u]);
+            if constexpr (kAdd) {
+                if (e0 + u < count && s_item[2 + e0 + u].x != it.x)
+                    load_old<kCols>(a, c, it.x, old[u]);
+            }
         }
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
@@ -416,11 +443,11 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(SumArgs a)
             const bool ends = s_item[2 + e0 + u].x != token;
             if (ends || e0 + u + 1 == count) {
                 if (entered)
-                    store_part<kCols, kAligned>(a, c, 2 * (int64_t)blockIdx.x, acc);
+                    store_part<kCols>(a, c, 2 * (int64_t)blockIdx.x, acc);
                 else if (ends)
-                    store_row<kCols, kAligned>(a, c, token, acc);
+                    store_row<kCols, kAdd>(a, c, token, acc, old[kAdd ? u : 0]);
                 else
-                    store_part<kCols, kAligned>(a, c, 2 * (int64_t)blockIdx.x + 1, acc);
+                    store_part<kCols>(a, c, 2 * (int64_t)blockIdx.x + 1, acc);
                 entered = false;
 #pragma unroll
                 for (int k = 0; k < kCols; ++k) acc[k] = 0.f;
@@ -429,9 +456,9 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(SumArgs a)
     }
 }
 
-// Runs that cross chunk borders: the block of the chunk where a run begins
-// adds up its partials in order.
-template <int kCols, bool kAligned>
+// Runs that cross chunk borders: the blocks of the chunk where a run begins
+// add up its partials in order, four columns per thread, 16 rows in flight.
+template <bool kAdd>
 __global__ __launch_bounds__(256) void embedding_join_kernel(SumArgs a)
 {
     const int32_t ch = blockIdx.x;
@@ -454,44 +481,33 @@ __global__ __launch_bounds__(256) void embedding_join_kernel(SumArgs a)
         }
         last += 64;
     }
-    const Columns<kCols, kAligned> c(a.hidden);
-    float acc[kCols];
-    auto part = [&](int64_t row, float (&x)[kCols]) {
-        const float* p = a.part + row * a.pld;
-        if constexpr (kAligned) {
-#pragma unroll
-            for (int k = 0; k < kCols; k += 4) {
-                const f32x4 y = c.has(0) ? *(const f32x4*)(p + c.first + k) : f32x4(0.f);
-#pragma unroll
-                for (int r = 0; r < 4; ++r) x[k + r] = y[r];
-            }
-        } else {
-#pragma unroll
-            for (int k = 0; k < kCols; ++k) x[k] = c.has(k) ? p[c.col(k)] : 0.f;
-        }
-    };
-    part(2 * (int64_t)ch + 1, acc);
-    constexpr int kAhead = 4;
+    const Columns<4> c(a.hidden);
+    if (c.count == 0) return;
+    const float* part = a.part + c.first;
+    f32x4 acc = *(const f32x4*)(part + (2 * (int64_t)ch + 1) * a.pld);
+    constexpr int kAhead = 16;
     for (int32_t k0 = ch + 1; k0 <= last; k0 += kAhead) {
-        float x[kAhead][kCols];
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u) part(2 * (int64_t)(k0 + u <= last ? k0 + u : k0), x[u]);
+        f32x4 x[kAhead];
 #pragma unroll
         for (int u = 0; u < kAhead; ++u)
-            if (k0 + u <= last)
+            x[u] = *(const f32x4*)(part + 2 * (int64_t)(k0 + u <= last ? k0 + u : k0) * a.pld);
 #pragma unroll
-                for (int k = 0; k < kCols; ++k) acc[k] += x[u][k];
+        for (int u = 0; u < kAhead; ++u)
+            if (k0 + u <= last) acc += x[u];
     }
-    store_row<kCols, kAligned>(a, c, token, acc);
+    const float sum[4] = {acc[0], acc[1], acc[2], acc[3]};
+    float old[4];
+    if constexpr (kAdd) load_old<4>(a, c, token, old);
+    store_row<4, kAdd>(a, c, token, sum, old);
 }
 
-// Entries per chunk: 32 (the partial rows then cost at most a 16th of the
-// reads), more for long lists, so that neither the chunks nor the partials of
-// one run become very many.
+// Entries per chunk: as few as 8 (a block's rows are a chain of latencies, so
+// short lists want many blocks), more for long lists, so that neither the
+// chunks, the partial rows nor the partials of one run become very many.
 int32_t chunk_entries(int64_t n)
 {
-    const int64_t c = round_up(div_up(n, 2048), 32);
-    return (int32_t)(c < 32 ? 32 : c > kMaxChunk ? kMaxChunk : c);
+    const int64_t c = round_up(div_up(n, 1024), 8);
+    return (int32_t)(c < 8 ? 8 : c > kMaxChunk ? kMaxChunk : c);
 }
 
 struct GradBuffers {
@@ -514,24 +530,25 @@ int64_t carve(int64_t n, int64_t vocab, int64_t hidden, void* ws, GradBuffers* b
 }
 
 template <typename T>
-hipError_t launch_sum(const SumArgs& a, bool aligned, hipStream_t st)
+hipError_t launch_sum(const SumArgs& a, hipStream_t st)
 {
     constexpr int kCols = Row<T>::kCols;
     int64_t threads = round_up(div_up(a.hidden, kCols), 64);
     if (threads > 256) threads = 256;
     const dim3 block((unsigned)threads);
     const unsigned slabs = (unsigned)div_up(a.hidden, threads * kCols);
-    const dim3 grid((unsigned)(a.chunks + a.zero_blocks), slabs), joins((unsigned)a.chunks, slabs);
-    if (aligned)
+    const dim3 grid((unsigned)(a.chunks + a.zero_blocks), slabs);
+    const dim3 joins((unsigned)a.chunks, (unsigned)div_up(a.hidden, 1024));
+    if (a.accumulate)
         embedding_sum_kernel<T, true><<<grid, block, 0, st>>>(a);
     else
         embedding_sum_kernel<T, false><<<grid, block, 0, st>>>(a);
-    hipError_t err = hipGetLastError();
+    const hipError_t err = hipGetLastError();
     if (err != hipSuccess || a.chunks < 2) return err;
-    if (aligned)
-        embedding_join_kernel<kCols, true><<<joins, block, 0, st>>>(a);
+    if (a.accumulate)
+        embedding_join_kernel<true><<<joins, dim3(256), 0, st>>>(a);
     else
-        embedding_join_kernel<kCols, false><<<joins, block, 0, st>>>(a);
+        embedding_join_kernel<false><<<joins, dim3(256), 0, st>>>(a);
     return hipGetLastError();
 }
 
@@ -573,16 +590,10 @@ hipError_t launch_grad(const void* grad, int32_t grad_type, int64_t grad_ld, con
     a.vocab = (int32_t)vocab;
     a.chunk = chunk_entries(n);
     a.chunks = (int32_t)div_up(n, a.chunk);
-    a.zero_blocks = accumulate ? 0 : (int32_t)(vocab < 2048 ? vocab : 2048);
+    a.zero_blocks = accumulate ? 0 : (int32_t)(vocab < 64 * 2048 ? div_up(vocab, 64) : 2048);
     a.out_f32 = out_type == DTE_TYPE_F32;
     a.accumulate = accumulate;
-    const int64_t cols = grad_type == DTE_TYPE_F32 ? 4 : 8;
-    const bool aligned = hidden % cols == 0 &&
-                         rows_aligned(grad, grad_ld, type_size(grad_type), 16) &&
-                         rows_aligned(out, out_ld, type_size(out_type),
-                                      out_type == DTE_TYPE_F32 ? 16 : 8);
-    return grad_type == DTE_TYPE_F32 ? launch_sum<float>(a, aligned, st)
-                                     : launch_sum<uint16_t>(a, aligned, st);
+    return grad_type == DTE_TYPE_F32 ? launch_sum<float>(a, st) : launch_sum<uint16_t>(a, st);
 }
 
 // Every row of the table zero (no ids).
