@@ -92,58 +92,51 @@ __device__ __forceinline__ double block_sum(double x, double* s)
     return (s[0] + s[1]) + (s[2] + s[3]);
 }
 
-// Four values of row r from column c; beyond the row zero.  kVec: rows begin
-// and end at 16-byte (binary32) or 8-byte (BF16) addresses.
-template <bool kVec>
+// Four values of row r from column c; beyond the row zero.
+__device__ __forceinline__ f32x4 load4(const float* p, int32_t left)
+{
+    f32x4 x = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (left >= 4) {
+        const f32x4_any y = *(const f32x4_any*)p;
+        x = f32x4{y[0], y[1], y[2], y[3]};
+    } else {
+#pragma unroll
+        for (int k = 0; k < 3; ++k)
+            if (k < left) x[k] = p[k];
+    }
+    return x;
+}
 __device__ __forceinline__ f32x4 values(const Source& s, int64_t b, int32_t r, int32_t c,
                                         int32_t rows, int32_t cols)
 {
-    f32x4 x = f32x4{0.f, 0.f, 0.f, 0.f};
+    const int32_t left = cols - c;
     if (s.momentum) {
         const int64_t at = (b * rows + r) * cols + c;
-        if constexpr (kVec) {
-            x = *(const f32x4*)(s.momentum + at);
-            if (s.nesterov) {
-                const f32x4 g = *(const f32x4*)(s.g + at);
+        f32x4 x = load4(s.momentum + at, left);
+        if (s.nesterov) {
+            const f32x4 g = load4(s.g + at, left);
 #pragma unroll
-                for (int k = 0; k < 4; ++k) x[k] = muon_value(s, x[k], g[k]);
-            }
-        } else {
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-                if (c + k < cols)
-                    x[k] = muon_value(s, s.momentum[at + k], s.nesterov ? s.g[at + k] : 0.f);
+            for (int k = 0; k < 4; ++k) x[k] = muon_value(s, x[k], g[k]);
         }
         return x;
     }
     const int64_t at = b * s.stride + r * s.ld + c;
-    if (s.bf16) {
-        const uint16_t* q = (const uint16_t*)s.x + at;
-        if constexpr (kVec) {
-            const uint2 w = *(const uint2*)q;
-            x = f32x4{from_bf16((uint16_t)w.x), from_bf16((uint16_t)(w.x >> 16)),
-                      from_bf16((uint16_t)w.y), from_bf16((uint16_t)(w.y >> 16))};
-        } else {
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-                if (c + k < cols) x[k] = from_bf16(q[k]);
-        }
+    if (!s.bf16) return load4((const float*)s.x + at, left);
+    const uint16_t* q = (const uint16_t*)s.x + at;
+    f32x4 x = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (left >= 4) {
+        const u16x4_any y = *(const u16x4_any*)q;
+        x = f32x4{from_bf16(y[0]), from_bf16(y[1]), from_bf16(y[2]), from_bf16(y[3])};
     } else {
-        const float* q = (const float*)s.x + at;
-        if constexpr (kVec) {
-            x = *(const f32x4*)q;
-        } else {
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-                if (c + k < cols) x[k] = q[k];
-        }
+        for (int k = 0; k < 3; ++k)
+            if (k < left) x[k] = from_bf16(q[k]);
     }
     return x;
 }
 
 // Partial sums of squares in binary64 (no overflow or underflow whatever the
 // matrix's scale); a Muon step's momentum is updated on the way.
-template <bool kVec>
 __global__ __launch_bounds__(256) void norm_kernel(Source s, int32_t rows, int32_t cols,
                                                    double* part)
 {
@@ -155,18 +148,16 @@ __global__ __launch_bounds__(256) void norm_kernel(Source s, int32_t rows, int32
         const int32_t r = (int32_t)(q / per), c = (int32_t)(q - r * per) * 4;
         if (s.momentum) {
             const int64_t at = (b * rows + r) * cols + c;
-            if constexpr (kVec) {
-                const f32x4 m = *(const f32x4*)(s.momentum + at) * s.mu +
-                                *(const f32x4*)(s.g + at);
-                *(f32x4*)(s.momentum + at) = m;
+            const f32x4 m = load4(s.momentum + at, cols - c) * s.mu + load4(s.g + at, cols - c);
+            if (c + 4 <= cols) {
+                *(f32x4_any*)(s.momentum + at) = f32x4_any{m[0], m[1], m[2], m[3]};
             } else {
 #pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    if (c + k < cols)
-                        s.momentum[at + k] = s.mu * s.momentum[at + k] + s.g[at + k];
+                for (int k = 0; k < 3; ++k)
+                    if (c + k < cols) s.momentum[at + k] = m[k];
             }
         }
-        const f32x4 u = values<kVec>(s, b, r, c, rows, cols);
+        const f32x4 u = values(s, b, r, c, rows, cols);
 #pragma unroll
         for (int k = 0; k < 4; ++k) sum += (double)u[k] * u[k];
     }
@@ -192,7 +183,6 @@ __device__ __forceinline__ Split4 split(f32x4 x)
                   make_uint2(pack(l[0], l[1]), pack(l[2], l[3]))};
 }
 // X_0 = x / (|x| + eps), padded with zeros to [rpad, cpad], scaled.
-template <bool kVec>
 __global__ __launch_bounds__(256) void normalise_kernel(Source s, int32_t rows, int32_t cols,
                                                         int32_t rpad, int32_t cpad,
                                                         const double* part, int32_t parts,
@@ -210,7 +200,7 @@ __global__ __launch_bounds__(256) void normalise_kernel(Source s, int32_t rows, 
     for (uint32_t q = blockIdx.x * 256 + threadIdx.x; q < n; q += gridDim.x * 256) {
         const int32_t r = (int32_t)(q / per), c = (int32_t)(q - r * per) * 4;
         f32x4 x = f32x4{0.f, 0.f, 0.f, 0.f};
-        if (r < rows && c < cols) x = values<kVec>(s, b, r, c, rows, cols) * inv;
+        if (r < rows && c < cols) x = values(s, b, r, c, rows, cols) * inv;
         const Split4 w = split(x * scale);
         *(uint2*)(hi + (int64_t)q * 4) = w.hi;
         *(uint2*)(lo + (int64_t)q * 4) = w.lo;
@@ -391,7 +381,6 @@ struct LastEpi {
         uint16_t* out;
         int64_t out_ld, out_stride;
         int32_t rows, cols;
-        int32_t vec;           // rows of out and p at 16-byte addresses
         float* p;              // [batch, rows, cols]
         float decay, rate;
     };
@@ -399,7 +388,7 @@ struct LastEpi {
         static constexpr bool kMirror = false, kAhead = !kMuon;   // (the registers it takes)
         struct Regs {
             typename LinearRows<kWide>::Regs x;
-            f32x4 p[kMuon ? 2 : 1];
+            f32x4_any p[kMuon ? 2 : 1];
         };
         const Args& e;
         LinearRows<kWide> lin;
@@ -411,10 +400,10 @@ struct LastEpi {
             if (jj >= e.rows || ii >= e.cols) return;
             lin.load(r.x, jj, ii);
             if constexpr (kMuon) {
-                if (e.vec && ii + 8 <= e.cols) {
-                    const float* q = p + jj * e.cols + ii;
-                    r.p[0] = *(const f32x4*)q;
-                    r.p[1] = *(const f32x4*)(q + 4);
+                if (ii + 8 <= e.cols) {
+                    const f32x4_any* q = (const f32x4_any*)(p + jj * e.cols + ii);
+                    r.p[0] = q[0];
+                    r.p[1] = q[1];
                 }
             }
         }
@@ -427,17 +416,17 @@ struct LastEpi {
             const uint32_t u[4] = {w.x, w.y, w.z, w.w};
             uint16_t* q = out + jj * e.out_ld + ii;
             float* v = kMuon ? p + jj * e.cols + ii : nullptr;
-            if (e.vec && ii + 8 <= e.cols) {
-                *(uint4*)q = w;
+            if (ii + 8 <= e.cols) {
+                store8(q, w);
                 if constexpr (kMuon) {
 #pragma unroll
                     for (int k = 0; k < 8; k += 4) {
-                        f32x4 y;
+                        f32x4_any y;
 #pragma unroll
                         for (int i = 0; i < 4; ++i)
                             y[i] = e.decay * r.p[k >> 2][i] -
                                    e.rate * from_bf16((uint16_t)(u[(k + i) >> 1] >> 16 * (i & 1)));
-                        *(f32x4*)(v + k) = y;
+                        *(f32x4_any*)(v + k) = y;
                     }
                 }
             } else {
@@ -612,16 +601,14 @@ hipError_t last_product(const pr::ProductArgs& u, const LinearTerm& x, const Ort
                         const Result& o, hipStream_t st)
 {
     constexpr pr::Layout kA = kWide ? pr::kR : pr::kK;
-    int32_t vec = rows_aligned(o.out, o.ld, 2, 16) && o.stride % 8 == 0;
     if (o.muon) {
-        vec = vec && rows_aligned(o.muon->p, z.cols, 4, 16) && z.rows * z.cols % 4 == 0;
         const typename LastEpi<kWide, true>::Args e{x, o.out, o.ld, o.stride, (int32_t)z.rows,
-                                                    (int32_t)z.cols, vec, o.muon->p,
+                                                    (int32_t)z.cols, o.muon->p,
                                                     o.muon->decay, o.muon->rate};
         return product<kA, pr::kK, LastEpi<kWide, true>>(u, e, st);
     }
     const typename LastEpi<kWide, false>::Args e{
-        x, o.out, o.ld, o.stride, (int32_t)z.rows, (int32_t)z.cols, vec, nullptr, 0.f, 0.f};
+        x, o.out, o.ld, o.stride, (int32_t)z.rows, (int32_t)z.cols, nullptr, 0.f, 0.f};
     return product<kA, pr::kK, LastEpi<kWide, false>>(u, e, st);
 }
 
@@ -706,24 +693,10 @@ hipError_t group(Source src, const OrthSizes& z, int64_t b0, int64_t batch,
     if (blocks > most) blocks = most;
     const dim3 xgrid((unsigned)blocks, (unsigned)batch);
     const int32_t rows = (int32_t)z.rows, cols = (int32_t)z.cols;
-    bool vec = cols % 4 == 0;
-    if (src.momentum)
-        vec = vec && rows_aligned(src.momentum, cols, 4, 16) && rows_aligned(src.g, cols, 4, 16);
-    else
-        vec = vec && rows_aligned(src.x, src.ld, src.bf16 ? 2 : 4, src.bf16 ? 8 : 16) &&
-              src.stride % 4 == 0;
-    const float xs = (float)fp16_scale(bd.sigma[0]);
-    if (vec) {
-        norm_kernel<true><<<ngrid, block, 0, st>>>(src, rows, cols, b.part);
-        normalise_kernel<true><<<xgrid, block, 0, st>>>(src, rows, cols, (int32_t)z.rpad,
-                                                        (int32_t)z.cpad, b.part, parts, ns.eps, xs,
-                                                        b.hi[0], b.lo);
-    } else {
-        norm_kernel<false><<<ngrid, block, 0, st>>>(src, rows, cols, b.part);
-        normalise_kernel<false><<<xgrid, block, 0, st>>>(src, rows, cols, (int32_t)z.rpad,
-                                                         (int32_t)z.cpad, b.part, parts, ns.eps,
-                                                         xs, b.hi[0], b.lo);
-    }
+    norm_kernel<<<ngrid, block, 0, st>>>(src, rows, cols, b.part);
+    normalise_kernel<<<xgrid, block, 0, st>>>(src, rows, cols, (int32_t)z.rpad, (int32_t)z.cpad,
+                                              b.part, parts, ns.eps,
+                                              (float)fp16_scale(bd.sigma[0]), b.hi[0], b.lo);
     const hipError_t err = hipGetLastError();
     if (err != hipSuccess) return err;
     return z.wide ? iterate<true>(z, batch, ns, bd, b, o, st)
