@@ -176,11 +176,17 @@ __global__ __launch_bounds__(kSortThreads) void sort_pass_kernel(SortPlan p, int
                                                                  int32_t* next_hist, int2* out,
                                                                  uint8_t* flags)
 {
-    __shared__ int32_t s_base[kMaxBins];                // next output place per digit
     __shared__ int32_t s_count[kSortWaves][kMaxBins];
     __shared__ int32_t s_wave[kSortWaves];
     const int32_t bins = 1 << p.bits;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+
+    const int32_t begin = blockIdx.x * p.per;
+    const int32_t end = p.n - begin < p.per ? p.n : begin + p.per;
+    auto item_at = [&](int32_t i) {
+        return i >= end ? make_int2(0, 0) : ids ? make_int2(key_of(ids, i, p.vocab), i) : in[i];
+    };
+    int2 item = item_at(begin + tid), after = item_at(begin + kSortThreads + tid);
 
     // totals of each digit, and its counts in the blocks before this one
     int32_t total = 0, before = 0;
@@ -203,54 +209,63 @@ __global__ __launch_bounds__(kSortThreads) void sort_pass_kernel(SortPlan p, int
     }
     if (lane == 63) s_wave[wave] = scan;
     for (int w = 0; w < kSortWaves; ++w)
-        for (int i = tid; i < bins; i += kSortThreads) s_count[w][i] = 0;
+        if (tid < bins) s_count[w][tid] = 0;
     __syncthreads();
-    int32_t base = scan - total + before;
+    int32_t base = scan - total + before;               // next output place of digit tid
     for (int w = 0; w < wave; ++w) base += s_wave[w];
-    if (tid < bins) s_base[tid] = base;
-    __syncthreads();
 
-    const int32_t begin = blockIdx.x * p.per;
-    const int32_t end = p.n - begin < p.per ? p.n : begin + p.per;
     for (int32_t first = begin; first < end; first += kSortThreads) {
-        const int32_t i = first + tid;
-        const bool live = i < end;
-        int2 item = make_int2(0, 0);
-        if (live) item = ids ? make_int2(key_of(ids, i, p.vocab), i) : in[i];
+        const bool live = first + tid < end;
+        const int2 later = item_at(first + 2 * kSortThreads + tid);
         const int32_t d = (item.x >> shift) & (bins - 1);
-        // lanes of the wave with the same digit
+        // lanes of the wave with the same digit, and with the same next one too
+        const int32_t d2 = (item.x >> (shift + p.bits)) & (bins - 1);
         uint64_t same = __ballot(live);
         for (int b = 0; b < p.bits; ++b) {
             const uint64_t set = __ballot((d >> b) & 1);
             same &= (d >> b) & 1 ? set : ~set;
         }
+        uint64_t same2 = same;
+        if (next_hist)
+            for (int b = 0; b < p.bits; ++b) {
+                const uint64_t set = __ballot((d2 >> b) & 1);
+                same2 &= (d2 >> b) & 1 ? set : ~set;
+            }
         const int rank = __popcll(same & ((1ull << lane) - 1));
         if (live && rank == 0) s_count[wave][d] = __popcll(same);
         __syncthreads();
         // exclusive over the waves, from the digit's next place
         if (tid < bins) {
-            int32_t run = s_base[tid];
 #pragma unroll
             for (int w = 0; w < kSortWaves; ++w) {
                 const int32_t c = s_count[w][tid];
-                s_count[w][tid] = run;
-                run += c;
+                s_count[w][tid] = base;
+                base += c;
             }
-            s_base[tid] = run;
         }
         __syncthreads();
         if (live) {
             const int32_t to = s_count[wave][d] + rank;
             out[to] = item;
-            if (next_hist)
-                atomicAdd(&next_hist[to / p.per * bins + ((item.x >> (shift + p.bits)) &
-                                                          (bins - 1))], 1);
+            if (next_hist) {
+                // the first lane counts for all (a frequent token's atomics would
+                // queue up), unless their places lie in two blocks
+                const int top = 63 - __builtin_clzll(same2), low = __builtin_ctzll(same2);
+                const int32_t at = to - rank;
+                const int32_t b0 = (at + __popcll(same & ((1ull << low) - 1))) / p.per;
+                const int32_t b1 = (at + __popcll(same & ((1ull << top) - 1))) / p.per;
+                if (b0 != b1)
+                    atomicAdd(&next_hist[to / p.per * bins + d2], 1);
+                else if (lane == low)
+                    atomicAdd(&next_hist[b0 * bins + d2], __popcll(same2));
+            }
             if (flags && item.x < p.vocab) flags[item.x] = 1;
         }
-        __syncthreads();
-        for (int w = 0; w < kSortWaves; ++w)
-            if (tid < bins) s_count[w][tid] = 0;
-        __syncthreads();
+        // back to zero for the next round: the wave's own counters, and its
+        // LDS operations are in order
+        for (int x = lane; x < bins; x += 64) s_count[wave][x] = 0;
+        item = after;
+        after = later;
     }
 }
 
