@@ -715,6 +715,7 @@ ShapeKind shape_for(int64_t ni, int64_t nj, int cus)
 }
 
 constexpr int64_t kPieceBytes = (int64_t)256 << 20;   // of G
+constexpr int64_t kMaxPiece = 1 << 21;                // G's row stride: an operand's (pr::kMaxLd)
 
 // Tiles of grad_hidden and how many blocks share a tile's vocabulary rows (few
 // tiles would leave CUs idle): the shape whose rounds take least, as in
@@ -774,6 +775,7 @@ bool sizes_of(const dte_linear_ce* c, bool backward, int32_t grad_type, Sizes* s
     }
     int64_t cols = s->tpad ? kPieceBytes / (s->tpad * 2 * s->terms) / 256 * 256 : 256;
     if (cols < 4096) cols = 4096;
+    if (cols > kMaxPiece) cols = kMaxPiece;
     if (s->pack) {
         int64_t most = kPieceBytes * 4 / (s->dpad * 2) / 256 * 256;
         if (most < 4096) most = 4096;

@@ -310,6 +310,33 @@ def test_linear_ce_pieces(T, V, d, dtype):
     within(gw, ex.dw, ex.dw_tol[dtype], "grad_weight")
 
 
+def test_linear_ce_of_few_tokens_over_a_very_large_vocabulary():
+    """More vocabulary than a row of one piece may have."""
+    T, V, d = 2, 4_300_000, 64
+    w = torch.zeros(V, d, dtype=torch.bfloat16, device="cuda")
+    at = torch.tensor([0, 1, 2097151, 2097152, 2097153, 4194303, 4194304, V - 1], device="cuda")
+    w[at] = randn(gen(1), len(at), d, dtype=torch.bfloat16)
+    h = randn(gen(2), T, d, dtype=torch.bfloat16)
+    target = torch.tensor([2097152, V - 1], device="cuda")
+    gl = torch.tensor([1.0, -0.5], device="cuda")
+    loss, lse = train.linear_ce(h, w, target)
+    z = torch.zeros(T, V, dtype=torch.float64, device="cuda")
+    z[:, at] = h.double() @ w[at].double().T.contiguous()
+    want = torch.logsumexp(z, 1)
+    assert float((lse - want).abs().max()) < 1e-4
+    gh, gw = train.linear_ce_grad(h, w, target, lse, gl,
+                                  torch.empty(V, d, dtype=torch.bfloat16, device="cuda"))
+    G = torch.exp(z - want[:, None])
+    G[torch.arange(T, device="cuda"), target] -= 1.0
+    G *= gl.double()[:, None]
+    rows = torch.cat([at, torch.tensor([17, 3_000_000], device="cuda")])
+    exact = G[:, rows].T.contiguous() @ h.double()
+    tol = 2.1 * UBF * (G[:, rows].T.contiguous().abs() @ h.double().abs()) + 1e-12
+    within(gw[rows], exact, tol, "grad_weight")
+    exact = G[:, at] @ w[at].double()
+    within(gh, exact, 2.1 * UBF * (G[:, at].abs() @ w[at].double().abs()) + 1e-9, "grad_hidden")
+
+
 def test_linear_ce_packed_forward_in_pieces():
     """More packed rows than one copy holds."""
     T, V, d = 3, 1_100_007, 65
