@@ -19,6 +19,12 @@
 // Padding tokens: the hidden states are copied once to a padded array in
 // which padding rows are zero, so whatever they hold stays out of grad_w;
 // their rows of G are zero.
+//
+// Bound by the matrix cores but for few tokens, where reading w is.  T 8192, V
+// 151936, d 4096, BF16 gradients: 30.4 ms (forward 7.4 ms, 1386 TFLOP/s; per
+// piece of 16384 vocabulary rows the logits and G 0.87 ms, 1270, grad_h 0.79
+// and grad_w 0.79 ms, 1390: the rate of a library product).  T 2048, d 2048,
+// binary32 grad_w (three terms: 12 T V d operations): 6.4 ms.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -150,7 +156,9 @@ struct StatsEpi {
 // (kPhase values); where that is not all, the sums of kRowGroups groups of rows wait
 // in registers for the next phase.  Statistics stay in registers until the
 // block ends: one pair per block and token.  Vocabulary 151936, 1 token of dim
-// 4096: 290 us with the tiles above.
+// 4096: 215 us, 5.8 TB/s (the tiles above: 280), 64 tokens of dim 2048: 124 us,
+// 5.0 TB/s (165; 150 with all blocks in the same phase, see below).  6 to 16
+// waves with 8 to 24 loads each: within 3 % for one token, 16 to 60 % slower for 64.
 constexpr int kStreamWaves = 8, kFlight = 16;
 constexpr int kStreamLds = 128 * 1024;
 
@@ -344,7 +352,8 @@ hipError_t stream_stats(StreamArgs a, int32_t blocks, hipStream_t st)
     }
 }
 
-// Joins the pairs of a token: `tok` tokens per block, 256 / tok lanes each.
+// Joins the pairs of a token: `tok` tokens per block, 256 / tok lanes each (4 us
+// for 64 tokens of 256 pairs, all of it latency; 13 us for 8192 of 594).
 __device__ __forceinline__ float2 join(float2 a, float2 b)
 {
     const float m = fmaxf(a.x, b.x), o = m == -INFINITY ? 0.f : m;
@@ -388,7 +397,8 @@ __global__ __launch_bounds__(256) void join_stats_kernel(const float2* part, int
 // ---- copies -----------------------------------------------------------------
 
 // dst[r, c] = src[r, c] for r < rows, c < cols, zero elsewhere in
-// [prows, pcols); rows whose target is padding are zero too.
+// [prows, pcols); rows whose target is padding are zero too.  (8192 x 4096: 23
+// us, 5.8 TB/s.)
 __global__ __launch_bounds__(256) void pad_rows_kernel(const uint16_t* src, int64_t ld,
                                                        int64_t rows, int64_t cols,
                                                        const int64_t* targets, int64_t vocab,
@@ -429,7 +439,11 @@ hipError_t pad_rows(const uint16_t* src, int64_t ld, int64_t rows, int64_t cols,
 
 // ---- backward: G of a piece ---------------------------------------------------
 
-// kTerms: BF16 terms that G is kept in.
+// kTerms: BF16 terms that G is kept in.  One where the results are BF16: its
+// rounding (2^-9 in the mean) is that of the result.  Three for a binary32
+// grad_w: 24 bits, so that what is left is the rounding of the sums (error
+// against binary64 5e-7; two terms would leave 3e-6, and FP16 terms would lose
+// small probabilities).
 template <int kTerms>
 struct GradEpi {
     struct Args {
@@ -638,7 +652,8 @@ struct WeightGradEpi {
 // grad_hidden = BF16 of the splits' sums, in the splits' order, and of the
 // part of the target's entry of G that its rounding took away: that entry is
 // often most of a token's gradient, and its exact product costs one row of
-// the weight.
+// the weight.  (8192 x 4096: 39 us, 6.9 TB/s, of 30 ms; the error of grad_h
+// against binary64 falls from 2.3e-3 to 1.7e-3, its own rounding.)
 __global__ __launch_bounds__(256) void hidden_grad_kernel(const float* part, int64_t stride,
                                                           int32_t splits, int64_t pld,
                                                           int64_t rows, int64_t cols,

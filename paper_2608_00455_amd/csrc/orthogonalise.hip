@@ -8,6 +8,12 @@
 // neither needs a transposed copy (product.h reads either orientation).  The
 // combinations are the products' epilogues.
 //
+// 128 matrices of 768 x 2048: 4.5 ms; per iteration S 212, B 120 and X 529 us
+// (the epilogue of X reads and writes 8 bytes per value, 1.6 GB, in bursts that
+// all CUs make at the same time).  One of 4096 x 4096, a whole Muon step: 1.43
+// ms; S 77, B 79, X 128 us (1070 TFLOP/s), norm and scaling 76 us.  One of 704
+// x 256: 153 us, 17 launches of 4 to 12 us that wait for one another.
+//
 // Precision: an iteration multiplies errors of weak singular directions by up
 // to a = 3.4, five of them by several hundred, so BF16 operands (8 bits) cost
 // percents of the result for matrices with a few strong directions.  Operands
