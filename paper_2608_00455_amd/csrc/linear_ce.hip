@@ -156,8 +156,8 @@ struct StatsEpi {
 // (kPhase values); where that is not all, the sums of kRowGroups groups of rows wait
 // in registers for the next phase.  Statistics stay in registers until the
 // block ends: one pair per block and token.  Vocabulary 151936, 1 token of dim
-// 4096: 215 us, 5.8 TB/s (the tiles above: 280), 64 tokens of dim 2048: 124 us,
-// 5.0 TB/s (165; 150 with all blocks in the same phase, see below).  6 to 16
+// 4096: 215 us, 5.8 TB/s (the tiles above: 231), 64 tokens of dim 2048: 124 us,
+// 5.0 TB/s (126; 150 with all blocks in the same phase, see below).  6 to 16
 // waves with 8 to 24 loads each: within 3 % for one token, 16 to 60 % slower for 64.
 constexpr int kStreamWaves = 8, kFlight = 16;
 constexpr int kStreamLds = 128 * 1024;
@@ -325,8 +325,9 @@ int32_t stream_blocks(int64_t n, int cus)
 template <int kJ, int kRowGroups>
 hipError_t launch_stream(const StreamArgs& a, int32_t blocks, hipStream_t st)
 {
+    static std::atomic<uint64_t> told{0};
     const hipError_t err = pr::allow_lds((const void*)stream_stats_kernel<kJ, kRowGroups>,
-                                         kStreamLds);
+                                         kStreamLds, told);
     if (err != hipSuccess) return err;
     stream_stats_kernel<kJ, kRowGroups>
         <<<dim3((unsigned)blocks), dim3(kStreamWaves * 64), kStreamLds, st>>>(a);
@@ -701,7 +702,7 @@ __global__ __launch_bounds__(256) void hidden_grad_kernel(const float* part, int
 
 // ---- the plan of a call ---------------------------------------------------------
 
-enum ShapeKind { kLarge, kMedium, kDeep, kThin64, kThin32 };
+enum ShapeKind { kLarge, kMedium, kDeep, kSmall };
 
 struct Sizes {
     int64_t T, V, d, tpad, dpad;
@@ -714,17 +715,21 @@ struct Sizes {
     bool stream;           // forward: few tokens
 };
 
-int tile_i(ShapeKind k) { return k == kMedium || k == kDeep ? 128 : 256; }
+int tile_i(ShapeKind k)
+{
+    return k == kSmall ? 64 : k == kMedium || k == kDeep ? 128 : 256;
+}
 
-// Tile shape of a product with ni x nj outputs: few j take the thin shapes,
-// which do not multiply rows that are not there.
+// Tile shape of a product with ni x nj outputs.  Few j take the small tiles, of
+// which the fewest rows are not there (256 x 64 and 256 x 32 tiles for them: as
+// fast at 151936 rows, up to 20 % slower at 16000).
 ShapeKind shape_for(int64_t ni, int64_t nj, int cus)
 {
-    if (nj <= 32) return kThin32;
-    if (nj <= 64) return kThin64;
+    if (nj <= 64) return kSmall;
     switch (pr::tiles_for(ni, nj, 1, false, false, cus)) {
     case pr::Tiles::kLarge: return kLarge;
     case pr::Tiles::kDeep: return kDeep;
+    case pr::Tiles::kSmall: return kSmall;
     default: return kMedium;
     }
 }
@@ -733,8 +738,10 @@ constexpr int64_t kPieceBytes = (int64_t)256 << 20;   // of G
 constexpr int64_t kMaxPiece = 1 << 21;                // G's row stride: an operand's (pr::kMaxLd)
 
 // Tiles of grad_hidden and how many blocks share a tile's vocabulary rows (few
-// tiles would leave CUs idle): the shape whose rounds take least, as in
-// pr::tiles_for, with at least 16 steps for each block.
+// tiles would leave CUs idle), with at least 16 steps for each block: small
+// tiles for few tokens and where one round holds them (301 tokens over 6002
+// rows, width 1024, both gradients: 49 -> 42 us), otherwise the shape whose
+// rounds take least, as in pr::tiles_for.
 void hidden_shape(Sizes* s, int cus)
 {
     const int64_t T = s->T > 0 ? s->T : 1, most = div_up(s->piece, 64 * 16);
@@ -742,13 +749,14 @@ void hidden_shape(Sizes* s, int cus)
         const int64_t x = slots / tiles;
         return x < 1 ? 1 : x > most ? most : x > 64 ? 64 : x;
     };
-    if (T <= 64) {
-        s->hid = T <= 32 ? kThin32 : kThin64;
-        s->split = (int32_t)split(div_up(s->d, 256), cus);
-        return;
-    }
     const int64_t tl = div_up(s->d, 256) * div_up(T, 256), sl = split(tl, cus);
     const int64_t tm = div_up(s->d, 128) * div_up(T, 128), sm = split(tm, 2 * cus);
+    const int64_t ts = div_up(s->d, 64) * div_up(T, 64), ss = split(ts, 2 * cus);
+    if (T <= 64 || (ts * ss <= 2 * cus && ss >= sm)) {
+        s->hid = kSmall;
+        s->split = (int32_t)ss;
+        return;
+    }
     const double large = (double)div_up(tl * sl, cus) / sl;
     const double medium = tm * sm <= cus ? 0.4 / sm : (double)div_up(tm * sm, 2 * cus) / sm * 0.62;
     s->hid = large <= medium ? kLarge : tm * sm <= cus ? kDeep : kMedium;
@@ -782,7 +790,11 @@ bool sizes_of(const dte_linear_ce* c, bool backward, int32_t grad_type, Sizes* s
             s->piece = rows < 256 ? 256 : rows;
             if (s->piece > s->V) s->piece = s->V;
         }
-        s->stream = s->T <= 64;
+        // Streaming costs 1 to 7 % less than tiles where every wave has several
+        // groups of rows, more where the last groups leave waves idle (64 tokens,
+        // width 4096: 8192 rows 45 us, tiles 20; 40000 rows 99, 81; one token,
+        // 40000 rows: 80, 85; 151936: 226, 242).
+        s->stream = s->T <= 64 && div_up(s->piece, 64) > (s->T <= 32 ? 2 : 8) * cus;
         s->parts = div_up(s->V, s->piece) *
                    (s->stream ? stream_blocks(s->piece, cus)
                               : div_up(s->piece, tile_i(s->logits)));
@@ -840,11 +852,7 @@ hipError_t product(ShapeKind k, const pr::ProductArgs& p, const typename Epi::Ar
     case kLarge: return pr::launch_product<pr::Large, false, kA, kB, Epi>(p, e, st);
     case kMedium: return pr::launch_product<pr::Medium, false, kA, kB, Epi>(p, e, st);
     case kDeep: return pr::launch_product<pr::Deep, false, kA, kB, Epi>(p, e, st);
-    default: break;
-    }
-    if constexpr (kB == pr::kK) {      // the thin shapes take a k-contiguous j operand only
-        if (k == kThin64) return pr::launch_product<pr::Thin64, false, kA, kB, Epi>(p, e, st);
-        return pr::launch_product<pr::Thin32, false, kA, kB, Epi>(p, e, st);
+    case kSmall: return pr::launch_product<pr::Small, false, kA, kB, Epi>(p, e, st);
     }
     return hipErrorInvalidValue;
 }

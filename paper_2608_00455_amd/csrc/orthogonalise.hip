@@ -12,7 +12,8 @@
 // (the epilogue of X reads and writes 8 bytes per value, 1.6 GB, in bursts that
 // all CUs make at the same time).  One of 4096 x 4096, a whole Muon step: 1.43
 // ms; S 77, B 79, X 128 us (1070 TFLOP/s), norm and scaling 76 us.  One of 704
-// x 256: 153 us, 17 launches of 4 to 12 us that wait for one another.
+// x 256: 92 us, 17 launches of 4 to 7 us that wait for one another (with tiles
+// of 128 x 128: 153).
 //
 // Precision: an iteration multiplies errors of weak singular directions by up
 // to a = 3.4, five of them by several hundred, so BF16 operands (8 bits) cost
@@ -289,6 +290,78 @@ struct SquareEpi {
     }
 };
 
+// A part of S, when several blocks share a tile's steps: the sums, in binary32.
+struct PartEpi {
+    struct Args {
+        float* out;            // [batch, split, ld, ld]
+        int64_t ld;
+    };
+    struct Rows {
+        static constexpr bool kMirror = false, kAhead = false;
+        struct Regs {};
+        float* out;
+        int64_t ld;
+        __device__ __forceinline__ void columns(int64_t) const {}
+        __device__ __forceinline__ void load(Regs&, int64_t, int64_t) const {}
+        __device__ __forceinline__ void put(const Regs&, int64_t jj, int64_t ii,
+                                            float (&x)[8]) const
+        {
+            if (jj >= ld || ii >= ld) return;
+            f32x4* q = (f32x4*)(out + jj * ld + ii);
+            q[0] = f32x4{x[0], x[1], x[2], x[3]};
+            q[1] = f32x4{x[4], x[5], x[6], x[7]};
+        }
+    };
+    template <class S>
+    static __device__ __forceinline__ void run(const Args& e, const pr::ProductArgs& p,
+                                               const pr::TileAt& at, const pr::LanePos<S>& pos,
+                                               f32x4 (&acc)[S::FI][S::FJ])
+    {
+        Rows f{e.out + ((int64_t)at.batch * p.split + at.split) * e.ld * e.ld, e.ld};
+        pr::for_rows<S>(pos, acc, f);
+    }
+};
+
+// S = scale * the sum of its parts, in their order, for a tile of 64 x 64 and
+// its mirror image.
+__global__ __launch_bounds__(256) void join_square_kernel(const float* part, int32_t split,
+                                                          int32_t ld, float scale, uint16_t* out)
+{
+    __shared__ uint16_t s_tile[64][72];
+    const int32_t ti = blockIdx.x, tj = blockIdx.y;
+    if (ti > tj) return;
+    const int64_t kk = (int64_t)ld * ld;
+    const int row = threadIdx.x >> 2, col = (threadIdx.x & 3) * 16;
+    const int64_t at = (int64_t)(tj * 64 + row) * ld + ti * 64 + col;
+    part += blockIdx.z * split * kk + at;
+    out += blockIdx.z * kk;
+    f32x4 x[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) x[k] = *(const f32x4*)(part + 4 * k);
+    for (int32_t s = 1; s < split; ++s) {
+        part += kk;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) x[k] += *(const f32x4*)(part + 4 * k);
+    }
+    float y[16];
+#pragma unroll
+    for (int k = 0; k < 16; ++k) y[k] = x[k >> 2][k & 3] * scale;
+    const uint4 a = f16x8(y), b = f16x8(y + 8);
+    *(uint4*)(out + at) = a;
+    *(uint4*)(out + at + 8) = b;
+    if (ti == tj) return;
+    *(uint4*)&s_tile[row][col] = a;
+    *(uint4*)&s_tile[row][col + 8] = b;
+    __syncthreads();
+    uint32_t w[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+        w[k] = pack(s_tile[col + 2 * k][row], s_tile[col + 2 * k + 1][row]);
+    uint16_t* q = out + (int64_t)(ti * 64 + row) * ld + tj * 64 + col;
+    *(uint4*)q = make_uint4(w[0], w[1], w[2], w[3]);
+    *(uint4*)(q + 8) = make_uint4(w[4], w[5], w[6], w[7]);
+}
+
 // What the epilogues of X' = (a + diag) X + B X share: X in two parts, and the
 // diagonal along the rows (kWide) or the columns.  The scales contain that of the
 // result.
@@ -514,7 +587,21 @@ struct OrthSizes {
     int64_t batch, rows, cols, rpad, cpad, kpad;
     int64_t group;         // matrices that are worked on together
     bool wide;
+    int32_t split;         // blocks that share a tile of S
 };
+
+// Small tiles of S that leave slots of the chip free share them: each tile's
+// steps along the longer side are split as far as the slots go, but not below
+// 6 steps, for joining the parts is a launch more (4 us, as long as 10 steps).
+// One matrix of 128 x 4096: 141 -> 106 us, of 768 x 4096: 209 -> 190.  (So the
+// number of matrices in a call decides about the order of these sums.)
+int32_t square_split(int64_t kpad, int64_t longer, int64_t batch, int cus)
+{
+    const int64_t t = kpad / 64, blocks = batch * t * (t + 1) / 2, steps = longer / 64;
+    int64_t split = 2 * cus / (blocks > 0 ? blocks : 1);
+    if (split > steps / 6) split = steps / 6;
+    return split >= 3 && split <= 64 ? (int32_t)split : split > 64 ? 64 : 1;
+}
 
 // Workspace of one matrix; and of all that are worked on together.  (Smaller
 // groups, whose work would stay in the 256 MiB last-level cache, leave the
@@ -543,13 +630,14 @@ bool orth_sizes(int64_t batch, int64_t rows, int64_t cols, OrthSizes* z)
     const int64_t bytes = work_bytes(*z);
     if (bytes > 0 && z->group > kGroupBytes / bytes) z->group = kGroupBytes / bytes;
     if (z->group < 1) z->group = 1;
+    z->split = square_split(z->kpad, z->wide ? z->cpad : z->rpad, z->group, device_cus());
     return true;
 }
 
 struct OrthBuffers {
     double* part;
     uint16_t *hi[2], *lo, *s, *b;
-    float* diag;
+    float *diag, *sums;
 };
 
 // Blocks per matrix that sum its squares: 4096 values each, until the chip is
@@ -573,6 +661,7 @@ int64_t carve(const OrthSizes& z, void* ws, OrthBuffers* b)
     b->s = c.take<uint16_t>(k);
     b->b = c.take<uint16_t>(k);
     b->diag = c.take<float>(z.group * z.kpad);
+    b->sums = c.take<float>(z.split > 1 ? z.group * z.split * z.kpad * z.kpad : 0);
     return c.used;
 }
 
@@ -586,6 +675,7 @@ hipError_t product(const pr::ProductArgs& p, const typename Epi::Args& e, hipStr
         if constexpr (kMiddle) return pr::launch_product<pr::Middle, true, kA, kB, Epi>(p, e, st);
         return hipErrorInvalidValue;       // (not chosen)
     case pr::Tiles::kDeep: return pr::launch_product<pr::Deep, true, kA, kB, Epi>(p, e, st);
+    case pr::Tiles::kSmall: return pr::launch_product<pr::Small, true, kA, kB, Epi>(p, e, st);
     case pr::Tiles::kMedium: break;
     }
     return pr::launch_product<pr::Medium, true, kA, kB, Epi>(p, e, st);
@@ -640,9 +730,22 @@ hipError_t iterate(const OrthSizes& z, int64_t batch, const dte_newton_schulz& n
         p.split = 1;
         p.batch = (int32_t)batch;
         p.symmetric = 1;
-        const SquareEpi<false>::Args eg{b.s, nullptr, nullptr, z.kpad, kk,
-                                        (float)(ss / (xs * xs)), 0.f, 0.f};
-        hipError_t err = product<kXrow, kXrow, SquareEpi<false>>(p, eg, st);
+        const float unit = (float)(ss / (xs * xs));
+        hipError_t err;
+        if (z.split > 1) {
+            p.split = z.split;
+            const PartEpi::Args eg{b.sums, z.kpad};
+            err = pr::launch_product<pr::Small, true, kXrow, kXrow, PartEpi>(p, eg, st);
+            if (err != hipSuccess) return err;
+            const unsigned t = (unsigned)(z.kpad / 64);
+            join_square_kernel<<<dim3(t, t, (unsigned)batch), 256, 0, st>>>(
+                b.sums, z.split, (int32_t)z.kpad, unit, b.s);
+            err = hipGetLastError();
+            p.split = 1;
+        } else {
+            const SquareEpi<false>::Args eg{b.s, nullptr, nullptr, z.kpad, kk, unit, 0.f, 0.f};
+            err = product<kXrow, kXrow, SquareEpi<false>>(p, eg, st);
+        }
         if (err != hipSuccess) return err;
         p.a = p.b = s;
         p.steps = (int32_t)(z.kpad / 64);

@@ -36,7 +36,7 @@
 //    a fragment read (16 bytes per lane, ds_read_b128) takes one chunk column
 //    of 16 rows, which the exclusive-or spreads over all banks.
 //  - row-contiguous: k is a row of 2*TR bytes; chunk c (8 rows) of k at
-//    position c ^ 2h(k), h(k) = (k & 3) | (bit 3 of k) << 2; a fragment is
+//    position c ^ 2h(k), h(k) = (k & 3) | (bit 3 of k) << 2 (spread()); a fragment is
 //    read with the transposing ds_read_b64_tr_b16 (each group of 16 lanes
 //    turns 4 k x 16 rows), whose 16 k-rows the exclusive-or spreads evenly.
 // The exclusive-or is applied to the global address of the load (the LDS side
@@ -119,6 +119,17 @@ __device__ __forceinline__ uint32_t lds_base()
 #endif
 }
 
+// Row-contiguous operands: a transposing read takes, of one k in four and of two
+// eights of k, 32 bytes each.  Pairs of 16-byte chunks are exchanged by k so
+// that these lie in different banks (64 rows are half the banks: k & 1 then
+// tells them apart already).
+template <int TR>
+__device__ __forceinline__ int spread(int k, int eight)
+{
+    static_assert(TR >= 64, "eight chunks per k");
+    return TR >= 128 ? k | eight << 2 : k >> 1 | eight << 1;
+}
+
 // Loads of one operand's tiles to LDS: TR rows x 64 k per step, kThreads
 // threads, kLoads 16-byte loads per thread.
 template <int TR, int kThreads, Layout kL>
@@ -159,13 +170,12 @@ struct TileLoader {
     {
         const int tid = threadIdx.x;
         constexpr int kChunks = TR / 8;
-        static_assert(kKC || kChunks >= 16, "the exclusive-or needs 16 chunks per row");
         const int last = (int)((o.rows - 1 - row0) >> 3);
         const int klast = kL == kRTail ? o.kvalid - 1 - s * kStepK : kStepK;
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
             const int q = i * kThreads + tid, k = q / kChunks, pos = q % kChunks;
-            const int c = pos ^ (2 * ((k & 3) | (((k >> 3) & 1) << 2)));
+            const int c = pos ^ (2 * spread<TR>(k & 3, k >> 3 & 1));
             off[i] = (uint32_t)((int64_t)(k < klast ? k : klast) * o.ld * 2) +
                      (c < last ? c : last) * 16;
         }
@@ -216,7 +226,7 @@ struct FragReader {
             at[0] = (w0 + j) * 128 + ((g ^ (l & 7)) * 16);
             at[1] = at[0] ^ 64;
         } else {
-            const int h = (j >> 2) | ((g & 1) << 2);
+            const int h = spread<TR>(j >> 2, g & 1);
 #pragma unroll
             for (int f = 0; f < kFrags; ++f)
                 at[f] = (g * 8 + (j >> 2)) * (TR * 2) +
@@ -294,8 +304,7 @@ typedef Shape<256, 256, 2, 4> Large;       // one block per CU
 typedef Shape<192, 192, 3, 4, 3> Middle;   // one block per CU, k-contiguous operands
 typedef Shape<128, 128, 2, 2> Medium;      // two blocks per CU
 typedef Shape<128, 128, 2, 2, 4> Deep;     // one block per CU
-typedef Shape<256, 64, 4, 1, 4> Thin64;    // few j: the i operand streams past
-typedef Shape<256, 32, 4, 1, 4> Thin32;
+typedef Shape<64, 64, 1, 4, 4> Small;      // two blocks per CU
 
 // The k loop.  On return the block's waves have left the loop together and no
 // load to LDS is in flight, so the epilogue may use all of the LDS.
@@ -503,10 +512,18 @@ __global__ __launch_bounds__(S::kThreads, S::kMinWaves) void product_kernel(Prod
 
 // More dynamic LDS than the default limit of 64 KiB: an attribute of the
 // function (a call of about a microsecond that changes nothing when repeated).
-inline hipError_t allow_lds(const void* kernel, int bytes)
+// Told to the runtime once per kernel and device (`told`: the kernel's own).
+inline hipError_t allow_lds(const void* kernel, int bytes, std::atomic<uint64_t>& told)
 {
     if (bytes <= 65536) return hipSuccess;
-    return hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    int device = 0;
+    hipError_t err = hipGetDevice(&device);
+    if (err != hipSuccess) return err;
+    const uint64_t bit = device < 64 ? (uint64_t)1 << device : 0;
+    if (told.load(std::memory_order_relaxed) & bit) return hipSuccess;
+    err = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (err == hipSuccess) told.fetch_or(bit, std::memory_order_relaxed);
+    return err;
 }
 
 template <class S, bool kF16, Layout kA, Layout kB, class Epi>
@@ -519,8 +536,9 @@ hipError_t launch_product(ProductArgs p, const typename Epi::Args& e, hipStream_
     const int64_t blocks = tiles * p.split * p.batch;
     if (blocks <= 0) return hipSuccess;
     if (blocks > 0x7fffffff) return hipErrorInvalidValue;
+    static std::atomic<uint64_t> told{0};
     const hipError_t err =
-        allow_lds((const void*)product_kernel<S, kF16, kA, kB, Epi>, S::kLds);
+        allow_lds((const void*)product_kernel<S, kF16, kA, kB, Epi>, S::kLds, told);
     if (err != hipSuccess) return err;
     hipLaunchKernelGGL((product_kernel<S, kF16, kA, kB, Epi>), dim3((unsigned)blocks),
                        dim3(S::kThreads), S::kLds, stream, p, e, (int32_t)(tiles * p.split));
@@ -533,8 +551,10 @@ hipError_t launch_product(ProductArgs p, const typename Epi::Args& e, hipStream_
 // two per CU (65 us; 0.4 with one per CU).  So large tiles are worth having
 // unless they leave much of the last round empty: the 136 tiles of a symmetric
 // 4096 x 4096 product fill half of one (97 us), its 253 middle ones all of
-// theirs (69 us).
-enum class Tiles { kLarge, kMiddle, kMedium, kDeep };
+// theirs (69 us).  Where one round holds all tiles of 64 x 64, latency is what
+// counts, and these take least of it: a product of 704 x 256 and K 256 6.4 us,
+// with tiles of 128 x 128 9.5 us, of 256 x 256 and K 704 7.7, 11.6.
+enum class Tiles { kLarge, kMiddle, kMedium, kDeep, kSmall };
 inline Tiles tiles_for(int64_t ni, int64_t nj, int64_t batch, bool symmetric, bool middle, int cus)
 {
     auto blocks = [&](int64_t t) {
@@ -544,6 +564,7 @@ inline Tiles tiles_for(int64_t ni, int64_t nj, int64_t batch, bool symmetric, bo
     auto rounds = [&](int64_t t, int64_t slots) {
         return (double)((blocks(t) + slots - 1) / slots);
     };
+    if (blocks(64) <= 2 * cus) return Tiles::kSmall;
     const double large = rounds(256, cus), mid = middle ? rounds(192, cus) * 0.65 : 1e30;
     const double medium = blocks(128) <= cus ? 0.4 : rounds(128, 2 * cus) * 0.62;
     if (large <= mid && large <= medium) return Tiles::kLarge;

@@ -310,6 +310,18 @@ def test_linear_ce_pieces(T, V, d, dtype):
     within(gw, ex.dw, ex.dw_tol[dtype], "grad_weight")
 
 
+@pytest.mark.parametrize("T,V,d,dtype", [
+    # few tokens: the weight streamed past them, or tiles of 64 x 64
+    (1, 40003, 192, torch.bfloat16), (20, 33000, 64, torch.float32),
+    (40, 100001, 64, torch.bfloat16), (64, 140000, 72, torch.bfloat16),
+    # tiles of 128 x 128, one and two per CU, and of 256 x 256
+    (520, 9000, 130, torch.float32), (700, 9000, 128, torch.bfloat16),
+    (2100, 7000, 1088, torch.bfloat16),
+])
+def test_linear_ce_tile_shapes(T, V, d, dtype):
+    test_linear_ce_pieces(T, V, d, dtype)
+
+
 def test_linear_ce_of_few_tokens_over_a_very_large_vocabulary():
     """More vocabulary than a row of one piece may have."""
     T, V, d = 2, 4_300_000, 64
@@ -472,6 +484,20 @@ def test_orthogonalise_large_tiles():
     for b in (0, 17, 39):
         want = exact_orth(x[b], [train.QUINTIC] * 5)
         assert float((out[b].double() - want).norm() / want.norm()) < ORTH_TOL
+
+
+@pytest.mark.parametrize("batch,rows,cols", [
+    (1, 16, 4096), (1, 5000, 60), (3, 200, 2050), (1, 130, 65535), (2, 1600, 300), (60, 64, 1300),
+])
+def test_orthogonalise_long_matrices(batch, rows, cols):
+    """Few small tiles of S, whose long sums several blocks share."""
+    say("case: orthogonalise", batch, rows, cols)
+    x = momentum_like(gen(rows + cols), batch, rows, cols, strong=8)
+    out = train.orthogonalise(x)
+    for b in range(0, batch, 7):
+        want = exact_orth(x[b], [train.QUINTIC] * 5)
+        assert float((out[b].double() - want).norm() / want.norm()) < ORTH_TOL
+    assert torch.equal(out, train.orthogonalise(x))
 
 
 def test_orthogonalise_scales_schedules_and_zeros():
