@@ -2,13 +2,13 @@
 // move memory: the forward reads and writes n rows, the gradient reads n rows
 // and writes the table (or reads and writes the rows that occur).  16384 rows
 // of 4096 in BF16: forward 36 us, 7.5 TB/s (rows of frequent tokens come from
-// the caches); gradient into a dense binary32 table of 151936 rows 560 us, of
-// which the sort takes 23, the sums and the zeros 523 (5.0 TB/s) and the joins
-// 19.  3001 rows of 1001 in binary32, added to a table: 27 us, five launches
-// of 2 to 9 us.
+// the caches); gradient into a dense binary32 table of 151936 rows 537 us, of
+// which the sort takes 23, the sums and the zeros 498 (5.2 TB/s) and the joins
+// 19.  3001 rows of 1001 in binary32, added to a table: 23 us, three launches
+// of 5 to 9 us.
 //
 // Gradient: the ids are sorted with their positions (stable radix sort, two
-// passes of 9 bits for a vocabulary below 2^18), so that a token's rows are
+// passes of 9 bits for a vocabulary below 2^18; short lists in one block), so that a token's rows are
 // consecutive and in ascending position.  The sorted list is cut into chunks
 // of equal length; a block sums the runs of its chunk in registers, one pass
 // over the rows.  A run that lies inside the chunk is finished there; a run
@@ -274,6 +274,110 @@ __global__ __launch_bounds__(kSortThreads) void sort_pass_kernel(SortPlan p, int
     }
 }
 
+// The whole sort in one block, for short lists and vocabularies of two digits
+// (12 bits of position and 18 of key in a word), where the kernels above are
+// three launches that wait for one another.  The gradient of 300 tokens, dim
+// 1024, added to a table: 20.6 -> 15.4 us; of 3001, dim 1001: 28.1 -> 23.4; of
+// 4096, dim 512: 24.7 -> 23.7; (of 8192, in 8 rounds: 28.3 -> 31.9).  A wave
+// owns consecutive items, 64 per round; its counters give an item its place
+// among the wave's, a scan over the waves and digits the wave's place.
+constexpr int kOneThreads = 1024, kOneWaves = kOneThreads / 64, kOneRounds = 4;
+constexpr int kOneItems = kOneThreads * kOneRounds, kOneBits = 12;
+static_assert(kOneItems == 1 << kOneBits, "positions");
+
+bool sorts_in_one(const SortPlan& p)
+{
+    return p.n <= kOneItems && p.bits * p.passes <= 18;
+}
+
+__global__ __launch_bounds__(kOneThreads) void sort_one_kernel(SortPlan p, const int64_t* ids,
+                                                               int2* out, uint32_t* flags,
+                                                               int32_t flag_words)
+{
+    __shared__ uint32_t s_item[kOneItems];
+    __shared__ uint16_t s_count[kOneWaves][kMaxBins];   // (counts of at most kOneItems)
+    __shared__ int32_t s_base[kMaxBins], s_wave[kOneWaves];
+    const int32_t bins = 1 << p.bits, rounds = (p.n + kOneThreads - 1) / kOneThreads;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int32_t first = wave * rounds * 64 + lane;
+    uint32_t v[kOneRounds];
+    int32_t off[kOneRounds];
+#pragma unroll
+    for (int r = 0; r < kOneRounds; ++r) {
+        const int32_t i = first + r * 64;
+        v[r] = r < rounds && i < p.n ? (uint32_t)key_of(ids, i, p.vocab) << kOneBits | i : 0;
+    }
+    for (int32_t i = tid; i < flag_words; i += kOneThreads) flags[i] = 0;
+    for (int k = 0; k < p.passes; ++k) {
+        const int shift = kOneBits + k * p.bits;
+        for (int x = lane; x < bins; x += 64) s_count[wave][x] = 0;
+        // (LDS operations of a wave are in order)
+        asm volatile("" ::: "memory");
+#pragma unroll
+        for (int r = 0; r < kOneRounds; ++r) {
+            if (r >= rounds) break;
+            const bool live = first + r * 64 < p.n;
+            const int32_t d = (v[r] >> shift) & (bins - 1);
+            uint64_t same = __ballot(live);
+            for (int b = 0; b < p.bits; ++b) {
+                const uint64_t set = __ballot((d >> b) & 1);
+                same &= (d >> b) & 1 ? set : ~set;
+            }
+            const int rank = __popcll(same & ((1ull << lane) - 1));
+            const int32_t prior = s_count[wave][d];
+            asm volatile("" ::: "memory");
+            off[r] = prior + rank;
+            if (live && rank == 0) s_count[wave][d] = (uint16_t)(prior + __popcll(same));
+            asm volatile("" ::: "memory");
+        }
+        __syncthreads();
+        int32_t total = 0;
+        if (tid < bins) {
+#pragma unroll
+            for (int w = 0; w < kOneWaves; ++w) {
+                const int32_t c = s_count[w][tid];
+                s_count[w][tid] = (uint16_t)total;
+                total += c;
+            }
+        }
+        int32_t scan = total;                           // inclusive over the digits
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int32_t up = __shfl_up(scan, d);
+            if (lane >= d) scan += up;
+        }
+        if (lane == 63) s_wave[wave] = scan;
+        __syncthreads();
+        if (tid < bins) {
+            int32_t base = scan - total;
+            for (int w = 0; w < wave; ++w) base += s_wave[w];
+            s_base[tid] = base;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < kOneRounds; ++r) {
+            if (r >= rounds) break;
+            const int32_t d = (v[r] >> shift) & (bins - 1);
+            if (first + r * 64 < p.n) s_item[s_base[d] + s_count[wave][d] + off[r]] = v[r];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < kOneRounds; ++r) {
+            const int32_t i = first + r * 64;
+            if (r < rounds && i < p.n) v[r] = s_item[i];
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < kOneRounds; ++r) {
+        const int32_t i = first + r * 64;
+        if (r >= rounds || i >= p.n) break;
+        const int32_t key = (int32_t)(v[r] >> kOneBits);
+        out[i] = make_int2(key, (int32_t)(v[r] & (kOneItems - 1)));
+        if (flag_words > 0 && key < p.vocab) ((uint8_t*)flags)[key] = 1;
+    }
+}
+
 // ---- summing the sorted rows ---------------------------------------------------
 
 constexpr int kMaxChunk = 1024;
@@ -286,7 +390,7 @@ struct SumArgs {
     const uint8_t* flags;  // null: accumulate
     int64_t grad_ld, out_ld, pld, hidden;
     float scale;
-    int32_t n, vocab, chunk, chunks, zero_blocks, out_f32, accumulate;
+    int32_t n, vocab, chunk, chunks, zero_blocks, zero_rows, out_f32, accumulate;
 };
 
 // kCols consecutive columns of a thread; `whole`: all of them exist.
@@ -376,16 +480,17 @@ __device__ __forceinline__ void store_row(const SumArgs& a, const Columns<kCols>
     }
 }
 
-// Zeros for the rows of tokens that do not occur: a wave looks at 64 flags at
-// once and writes the rows 1 KB at a time.  (Stores past the caches are no
-// faster: 151936 x 4096 in binary32, of which 16384 rows occur at most, 525 us
-// either way, 5.0 TB/s.)
+// Zeros for the rows of tokens that do not occur: a wave looks at zero_rows <=
+// 64 flags at once and writes the rows 1 KB at a time.  (Stores past the caches
+// are no faster: 151936 x 4096 in binary32, of which 16384 rows occur at most,
+// 525 us either way with 64 rows per wave.)
 __device__ __forceinline__ void zero_rows(const SumArgs& a, int64_t wave, int64_t waves)
 {
     const int lane = threadIdx.x & 63;
     const int64_t size = a.out_f32 ? 4 : 2, bytes = a.hidden * size;
-    for (int64_t v0 = wave * 64; v0 < a.vocab; v0 += waves * 64) {
-        uint64_t todo = __ballot(v0 + lane < a.vocab && !a.flags[v0 + lane]);
+    for (int64_t v0 = wave * a.zero_rows; v0 < a.vocab; v0 += waves * a.zero_rows) {
+        uint64_t todo = __ballot(lane < a.zero_rows && v0 + lane < a.vocab &&
+                                 !a.flags[v0 + lane]);
         while (todo) {
             const int64_t v = v0 + __builtin_ctzll(todo);
             todo &= todo - 1;
@@ -572,31 +677,47 @@ hipError_t launch_sum(const SumArgs& a, hipStream_t st)
     return hipGetLastError();
 }
 
-hipError_t launch_grad(const void* grad, int32_t grad_type, int64_t grad_ld, const int64_t* ids,
-                       int64_t n, int64_t vocab, int64_t hidden, float scale, void* out,
-                       int32_t out_type, int64_t out_ld, bool accumulate, const GradBuffers& b,
-                       hipStream_t st)
+// The sort of long lists; `words` of the flags are cleared and set.
+hipError_t sort(const SortPlan& p, const int64_t* ids, int64_t words, const GradBuffers& b,
+                hipStream_t st)
 {
-    const SortPlan p = sort_plan(n, vocab);
     const int64_t bins = (int64_t)1 << p.bits, per_pass = p.blocks * bins;
-    const int64_t words = accumulate ? 0 : div_up(vocab, 4);
     const int64_t clear = (p.passes - 1) * per_pass + words;
     int64_t blocks = div_up(clear, 4 * kSortThreads);
     blocks = blocks < p.blocks ? p.blocks : blocks > 1024 ? 1024 : blocks;
     sort_count_kernel<<<dim3((unsigned)blocks), dim3(kSortThreads), 0, st>>>(
         p, ids, b.hist, b.hist + per_pass, (p.passes - 1) * per_pass, b.flags, words);
     hipError_t err = hipGetLastError();
-    if (err != hipSuccess) return err;
-    for (int k = 0; k < p.passes; ++k) {
+    for (int k = 0; k < p.passes && err == hipSuccess; ++k) {
         sort_pass_kernel<<<dim3((unsigned)p.blocks), dim3(kSortThreads), 0, st>>>(
             p, k * p.bits, k == 0 ? ids : nullptr, k == 0 ? nullptr : b.pairs[(k + 1) & 1],
             b.hist + k * per_pass, k + 1 < p.passes ? b.hist + (k + 1) * per_pass : nullptr,
-            b.pairs[k & 1], k == 0 && !accumulate ? (uint8_t*)b.flags : nullptr);
+            b.pairs[k & 1], k == 0 && words > 0 ? (uint8_t*)b.flags : nullptr);
         err = hipGetLastError();
+    }
+    return err;
+}
+
+hipError_t launch_grad(const void* grad, int32_t grad_type, int64_t grad_ld, const int64_t* ids,
+                       int64_t n, int64_t vocab, int64_t hidden, float scale, void* out,
+                       int32_t out_type, int64_t out_ld, bool accumulate, const GradBuffers& b,
+                       hipStream_t st)
+{
+    const SortPlan p = sort_plan(n, vocab);
+    const int64_t words = accumulate ? 0 : div_up(vocab, 4);
+    hipError_t err;
+    const bool one = sorts_in_one(p);
+    if (one) {
+        sort_one_kernel<<<dim3(1), dim3(kOneThreads), 0, st>>>(p, ids, b.pairs[0], b.flags,
+                                                               (int32_t)words);
+        err = hipGetLastError();
+        if (err != hipSuccess) return err;
+    } else {
+        err = sort(p, ids, words, b, st);
         if (err != hipSuccess) return err;
     }
     SumArgs a;
-    a.sorted = b.pairs[(p.passes - 1) & 1];
+    a.sorted = b.pairs[one ? 0 : (p.passes - 1) & 1];
     a.grad = grad;
     a.out = out;
     a.part = b.part;
@@ -610,7 +731,13 @@ hipError_t launch_grad(const void* grad, int32_t grad_type, int64_t grad_ld, con
     a.vocab = (int32_t)vocab;
     a.chunk = chunk_entries(n);
     a.chunks = (int32_t)div_up(n, a.chunk);
-    a.zero_blocks = accumulate ? 0 : (int32_t)(vocab < 64 * 2048 ? div_up(vocab, 64) : 2048);
+    // rows of zeros per wave: few enough that 8192 waves have some (64 for every
+    // wave: 16 tokens, table 6002 x 1001 28.6 us, so 16.3; 16384 tokens, 151936 x
+    // 4096 561, so 537)
+    a.zero_rows = 64;
+    while (a.zero_rows > 1 && vocab < a.zero_rows * 8192) a.zero_rows /= 2;
+    const int64_t zero_blocks = div_up(vocab, 4 * a.zero_rows);
+    a.zero_blocks = accumulate ? 0 : (int32_t)(zero_blocks < 2048 ? zero_blocks : 2048);
     a.out_f32 = out_type == DTE_TYPE_F32;
     a.accumulate = accumulate;
     return grad_type == DTE_TYPE_F32 ? launch_sum<float>(a, st) : launch_sum<uint16_t>(a, st);

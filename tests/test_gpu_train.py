@@ -135,6 +135,15 @@ def test_embedding_grad(gdtype, tdtype, accumulate, vocab, hidden, n, pad, offse
     check_embedding_grad(vocab, hidden, n, gdtype, tdtype, accumulate, pad, offset)
 
 
+@pytest.mark.parametrize("vocab", [511, 512, 6002, 151936, 262143, 262144])
+@pytest.mark.parametrize("n", [63, 1023, 4095, 4096, 4097, 8192, 8193, 20001])
+def test_embedding_grad_sorts(vocab, n):
+    """Lists that one block sorts and longer ones, one to three digits."""
+    say("case: embedding_grad sorts", vocab, n)
+    check_embedding_grad(vocab, 4, n, torch.float32, torch.float32, False)
+    check_embedding_grad(vocab, 4, n, torch.float32, torch.float32, True)
+
+
 @pytest.mark.parametrize("n", [31, 32, 33, 64, 2500, 131072 + 17])
 def test_embedding_grad_of_one_token(n):
     """Runs that fill chunks exactly, cross every border, and lie between
