@@ -16,9 +16,10 @@
 // operations instead of 6 for the two directions together, and G of a piece
 // (rather than T x V logits) is all that is kept.
 //
-// Padding tokens: the hidden states are copied once to a padded array in
-// which padding rows are zero, so whatever they hold stays out of grad_w;
-// their rows of G are zero.
+// Padding tokens: backward copies the hidden states once to a padded array in
+// which padding rows are zero, so whatever they hold stays out of grad_w; their
+// rows of G are zero.  Forward reads the states in place where it can: no token
+// sees another's.
 //
 // Bound by the matrix cores but for few tokens, where reading w is.  T 8192, V
 // 151936, d 4096, BF16 gradients: 30.4 ms (forward 7.4 ms, 1386 TFLOP/s; per
@@ -164,11 +165,11 @@ constexpr int kStreamLds = 128 * 1024;
 
 struct StreamArgs {
     const uint16_t* w;
-    const uint16_t* h;     // [64][dpad]
+    const uint16_t* h;
     const int64_t* targets;
     float2* part;
     float* target_z;
-    int64_t ld, dpad, tpad, v0;
+    int64_t ld, hld, dpad, tpad, v0;
     int32_t n, tokens, part0, phase;   // rows; phase: of dim, a multiple of 64
     float scale;
 };
@@ -220,7 +221,8 @@ __global__ __launch_bounds__(kStreamWaves * 64, 2) void stream_stats_kernel(Stre
                 for (int32_t x = threadIdx.x; x < 16 * kJ * chunks; x += kStreamWaves * 64) {
                     const int32_t r = x / chunks, c = x - r * chunks;
                     *(DTE_LDS(s16x8)*)(uintptr_t)(lds + (r * chunks + (c ^ (r & 7))) * 16) =
-                        *(const s16x8*)(a.h + r * a.dpad + k0 + c * 8);
+                        *(const s16x8*)(a.h + (r < a.tokens ? r : a.tokens - 1) * a.hld + k0 +
+                                        c * 8);
                 }
                 __syncthreads();
             }
@@ -707,6 +709,7 @@ enum ShapeKind { kLarge, kMedium, kDeep, kSmall };
 struct Sizes {
     int64_t T, V, d, tpad, dpad;
     bool pack;             // weight rows are copied to padded, aligned rows
+    bool pack_h;           // so are the hidden states
     int64_t piece;         // vocabulary rows per piece
     int64_t gld;           // columns of G's rows
     int32_t terms, split;
@@ -780,6 +783,8 @@ bool sizes_of(const dte_linear_ce* c, bool backward, int32_t grad_type, Sizes* s
     s->dpad = round_up(s->d, 64);
     // the products load 16 bytes at 16-byte addresses and whole steps of 64
     s->pack = s->d % 64 != 0 || !rows_aligned(c->weight, c->weight_ld, 2, 16);
+    // (backward: and without what padding tokens hold, which grad_w must not see)
+    s->pack_h = backward || s->d % 64 != 0 || !rows_aligned(c->hidden, c->hidden_ld, 2, 16);
     s->logits = shape_for(s->V, s->T, cus);
     s->terms = backward && grad_type == DTE_TYPE_F32 ? 3 : 1;
     if (!backward) {
@@ -819,7 +824,7 @@ bool sizes_of(const dte_linear_ce* c, bool backward, int32_t grad_type, Sizes* s
 }
 
 struct Buffers {
-    uint16_t* h;           // [tpad][dpad]
+    uint16_t* h;           // [tpad][dpad] (pack_h)
     uint16_t* w;           // [piece][dpad] (pack)
     float2* part;          // forward
     float* target_z;
@@ -831,7 +836,7 @@ struct Buffers {
 int64_t carve(const Sizes& s, bool backward, void* ws, Buffers* b)
 {
     Carver c(ws);
-    b->h = c.take<uint16_t>(s.tpad * s.dpad);
+    b->h = s.pack_h ? c.take<uint16_t>(s.tpad * s.dpad) : nullptr;
     b->w = s.pack ? c.take<uint16_t>(s.piece * s.dpad) : nullptr;
     if (!backward) {
         b->part = c.take<float2>(s.parts * s.tpad);
@@ -862,29 +867,40 @@ pr::Operand operand(const uint16_t* p, int64_t ld, int64_t rows, int64_t kvalid,
     return pr::Operand{p, ld, 0, (int32_t)rows, (int32_t)kvalid, wrap};
 }
 
-// Rows [v0, v0 + n) of the weight as an operand's memory.
-struct WeightRows {
+// Rows of the hidden states, or [v0, v0 + n) of the weight, as an operand's memory.
+struct MatrixRows {
     const uint16_t* p;
     int64_t ld;
 };
 
+hipError_t hidden_rows(const dte_linear_ce* c, const Sizes& s, const Buffers& b, hipStream_t st,
+                       MatrixRows* h)
+{
+    if (!s.pack_h) {
+        *h = MatrixRows{c->hidden, c->hidden_ld};
+        return hipSuccess;
+    }
+    *h = MatrixRows{b.h, s.dpad};
+    return pad_rows(c->hidden, c->hidden_ld, s.T, s.d, c->targets, s.V, b.h, s.tpad, s.dpad, st);
+}
+
 hipError_t weight_rows(const dte_linear_ce* c, const Sizes& s, const Buffers& b, int64_t v0,
-                       int64_t n, hipStream_t st, WeightRows* w)
+                       int64_t n, hipStream_t st, MatrixRows* w)
 {
     const uint16_t* src = c->weight + v0 * c->weight_ld;
     if (!s.pack) {
-        *w = WeightRows{src, c->weight_ld};
+        *w = MatrixRows{src, c->weight_ld};
         return hipSuccess;
     }
-    *w = WeightRows{b.w, s.dpad};
+    *w = MatrixRows{b.w, s.dpad};
     return pad_rows(src, c->weight_ld, n, s.d, nullptr, 0, b.w, n, s.dpad, st);
 }
 
-pr::ProductArgs logits_product(const Sizes& s, const Buffers& b, const WeightRows& w, int64_t n)
+pr::ProductArgs logits_product(const Sizes& s, const MatrixRows& h, const MatrixRows& w, int64_t n)
 {
     pr::ProductArgs p{};
     p.a = operand(w.p, w.ld, n, 0);
-    p.b = operand(b.h, s.dpad, s.tpad, 0);
+    p.b = operand(h.p, h.ld, s.T, 0);
     p.ni = (int32_t)n;
     p.nj = (int32_t)s.tpad;
     p.steps = (int32_t)(s.dpad / 64);
@@ -901,21 +917,22 @@ pr::ProductArgs logits_product(const Sizes& s, const Buffers& b, const WeightRow
 dte_status forward(const dte_linear_ce* c, const Sizes& s, const Buffers& b, float* loss,
                    float* lse, hipStream_t st)
 {
-    DTE_TRY(pad_rows(c->hidden, c->hidden_ld, s.T, s.d, c->targets, s.V, b.h, s.tpad, s.dpad, st));
+    MatrixRows h;
+    DTE_TRY(hidden_rows(c, s, b, st, &h));
     int32_t part0 = 0;
     for (int64_t v0 = 0; v0 < s.V; v0 += s.piece) {
         const int64_t n = s.V - v0 < s.piece ? s.V - v0 : s.piece;
-        WeightRows w;
+        MatrixRows w;
         DTE_TRY(weight_rows(c, s, b, v0, n, st, &w));
         if (s.stream) {
             const int32_t blocks = stream_blocks(n, device_cus());
-            const StreamArgs a{w.p, b.h, c->targets, b.part, b.target_z, w.ld, s.dpad, s.tpad, v0,
-                               (int32_t)n, (int32_t)s.T, part0, 0, c->scale};
+            const StreamArgs a{w.p, h.p, c->targets, b.part, b.target_z, w.ld, h.ld, s.dpad,
+                               s.tpad, v0, (int32_t)n, (int32_t)s.T, part0, 0, c->scale};
             DTE_TRY(stream_stats(a, blocks, st));
             part0 += blocks;
             continue;
         }
-        const pr::ProductArgs p = logits_product(s, b, w, n);
+        const pr::ProductArgs p = logits_product(s, h, w, n);
         const StatsEpi::Args e{c->targets, b.part, b.target_z, s.tpad, (int32_t)s.T, s.V, v0,
                                part0,      c->scale};
         DTE_TRY((product<pr::kK, pr::kK, StatsEpi>(s.logits, p, e, st)));
@@ -933,13 +950,14 @@ dte_status backward(const dte_linear_ce* c, const Sizes& s, const Buffers& b, co
                     int64_t gw_ld, int32_t accumulate, hipStream_t st)
 {
     const int64_t size = type_size(type);
-    DTE_TRY(pad_rows(c->hidden, c->hidden_ld, s.T, s.d, c->targets, s.V, b.h, s.tpad, s.dpad, st));
+    MatrixRows h;
+    DTE_TRY(hidden_rows(c, s, b, st, &h));
     for (int64_t v0 = 0; v0 < s.V; v0 += s.piece) {
         const int64_t n = s.V - v0 < s.piece ? s.V - v0 : s.piece;
-        WeightRows w;
+        MatrixRows w;
         DTE_TRY(weight_rows(c, s, b, v0, n, st, &w));
         {
-            const pr::ProductArgs p = logits_product(s, b, w, n);
+            const pr::ProductArgs p = logits_product(s, h, w, n);
             auto grad = [&](auto terms) {
                 typedef GradEpi<decltype(terms)::value> Epi;
                 const typename Epi::Args e{c->targets, lse,    grad_loss, b.g,
@@ -965,7 +983,7 @@ dte_status backward(const dte_linear_ce* c, const Sizes& s, const Buffers& b, co
         if (gw) {
             pr::ProductArgs p{};
             const int32_t tsteps = (int32_t)(s.tpad / 64);
-            p.a = operand(b.h, s.dpad, s.dpad, s.tpad, s.terms > 1 ? tsteps : 0);
+            p.a = operand(h.p, h.ld, s.dpad, s.tpad, s.terms > 1 ? tsteps : 0);
             p.b = operand(b.g, s.gld, s.gld, s.terms * s.tpad);
             p.ni = (int32_t)s.d;
             p.nj = (int32_t)n;
