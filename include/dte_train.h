@@ -116,8 +116,10 @@ dte_status dte_linear_ce_forward(const dte_linear_ce* c, float* loss, float* lse
  *   G[t, v] = scale * grad_loss[t] * (exp(z[t, v] - lse[t]) - [v == targets[t]])
  *   grad_hidden = G weight,  grad_weight = G^T hidden
  * z is computed again, piece by piece of the vocabulary.  G is rounded to
- * BF16 once where the result is BF16; for a binary32 grad_weight it is kept
- * in three BF16 terms (24 bits).  Sums are in binary32.
+ * BF16 once where the result is BF16 (two BF16 terms for a grad_weight of at
+ * most 64 tokens); for a binary32 grad_weight it is kept in three BF16 terms
+ * (24 bits).  Sums are in binary32.  The probabilities' relative error is the
+ * rounding of z - lse, with lse in binary32: 1e-6 where lse is between 16 and 32.
  * lse: as dte_linear_ce_forward wrote it; grad_loss: float[tokens].
  * grad_hidden: BF16 [tokens, dim], zero for padding; grad_weight: [vocab,
  * dim] of grad_type, every element written; with accumulate != 0 (F32 only)

@@ -392,9 +392,10 @@ __global__ __launch_bounds__(256) void join_stats_kernel(const float2* part, int
     }
     if (y != 0 || t >= tokens) return;
     const bool ok = is_target(targets[t], vocab);
-    const float l = a.x + __builtin_amdgcn_logf(a.y) * kLn2;
-    lse[t] = ok ? l : 0.f;
-    loss[t] = ok ? l - target_z[t] : 0.f;
+    // (the loss not from lse: that is rounded to the last bit of the largest logit)
+    const float l = __builtin_amdgcn_logf(a.y) * kLn2;
+    lse[t] = ok ? a.x + l : 0.f;
+    loss[t] = ok ? a.x - target_z[t] + l : 0.f;
 }
 
 // ---- copies -----------------------------------------------------------------
@@ -443,7 +444,9 @@ hipError_t pad_rows(const uint16_t* src, int64_t ld, int64_t rows, int64_t cols,
 // ---- backward: G of a piece ---------------------------------------------------
 
 // kTerms: BF16 terms that G is kept in.  One where the results are BF16: its
-// rounding (2^-9 in the mean) is that of the result.  Three for a binary32
+// rounding (2^-9 in the mean) is that of the result (error 2.3e-3 where the
+// result's own rounding is 1.7e-3; up to 2.7e-3 for few tokens, so two there:
+// 1.7e-3).  Three for a binary32
 // grad_w: 24 bits, so that what is left is the rounding of the sums (error
 // against binary64 5e-7; two terms would leave 3e-6, and FP16 terms would lose
 // small probabilities).
@@ -737,6 +740,11 @@ ShapeKind shape_for(int64_t ni, int64_t nj, int cus)
     }
 }
 
+// Up to so many tokens a BF16 grad_w has a second term of G: their roundings are
+// too few to average out, and it costs little beside reading and writing the
+// vocabulary's rows (64 tokens, 151936 x 2048: 498 -> 543 us; 256: 710 -> 831).
+constexpr int64_t kFewTokens = 64;
+
 constexpr int64_t kPieceBytes = (int64_t)256 << 20;   // of G
 constexpr int64_t kMaxPiece = 1 << 21;                // G's row stride: an operand's (pr::kMaxLd)
 
@@ -786,7 +794,7 @@ bool sizes_of(const dte_linear_ce* c, bool backward, int32_t grad_type, Sizes* s
     // (backward: and without what padding tokens hold, which grad_w must not see)
     s->pack_h = backward || s->d % 64 != 0 || !rows_aligned(c->hidden, c->hidden_ld, 2, 16);
     s->logits = shape_for(s->V, s->T, cus);
-    s->terms = backward && grad_type == DTE_TYPE_F32 ? 3 : 1;
+    s->terms = !backward ? 1 : grad_type == DTE_TYPE_F32 ? 3 : s->T <= kFewTokens ? 2 : 1;
     if (!backward) {
         // the whole vocabulary at once, or what the packed copy has room for
         s->piece = s->V;
@@ -965,8 +973,9 @@ dte_status backward(const dte_linear_ce* c, const Sizes& s, const Buffers& b, co
                                            s.tpad,     v0,     s.V, (int32_t)s.T, c->scale};
                 return product<pr::kK, pr::kK, Epi>(s.logits, p, e, st);
             };
-            DTE_TRY(s.terms == 1 ? grad(std::integral_constant<int, 1>())
-                                 : grad(std::integral_constant<int, 3>()));
+            DTE_TRY(s.terms == 1   ? grad(std::integral_constant<int, 1>())
+                    : s.terms == 2 ? grad(std::integral_constant<int, 2>())
+                                   : grad(std::integral_constant<int, 3>()));
         }
         if (gh) {
             pr::ProductArgs p{};
