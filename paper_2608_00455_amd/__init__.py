@@ -3,8 +3,9 @@
 The compute path is libdte.so (HIP kernels for gfx950 behind the C ABI of
 include/dte.h).  This package holds its ctypes binding (`binding`, same
 names as the C entry points), the transfer-plan builder for the receiver
-layouts (`layouts`), and `pipeline`, which owns device buffers (allocated
-with torch) and chains the three hot calls.  There is no CPU fallback: if
+layouts (`layouts`), `pipeline`, which owns device buffers (allocated
+with torch) and chains the three hot calls, and `train`, the operators beside
+it that make the trainer's step (include/dte_train.h).  There is no CPU fallback: if
 libdte.so is missing, every entry point raises.
 """
 from .binding import (DTE_ERR_ARG, DTE_ERR_CAPACITY, DTE_ERR_HIP, DTE_ERR_PLAN,  # noqa: F401
