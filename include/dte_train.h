@@ -150,7 +150,9 @@ int64_t dte_orthogonalise_workspace_bytes(int64_t batch, int64_t rows, int64_t c
 /* Orthogonalise a batch of matrices: out[b] = X_steps of x[b].
  * Products run on FP16 operands (11 bits, scaled by powers of two that the
  * bound on the singular values gives) with binary32 sums; X itself is kept
- * in binary32 from step to step.  The Frobenius norm is summed in binary64.
+ * in two FP16 parts (21 bits) from step to step.  The Frobenius norm is summed
+ * in binary64.  The order of all sums depends on the sizes, the number of
+ * matrices among them, and on nothing else.
  * x: [batch, rows, cols] of x_type, strides x_ld and x_stride (elements
  * between matrices); out: BF16 likewise, rounded once.  rows, cols below
  * 2^16; batch below 2^16.  A zero matrix stays zero (with eps > 0).
